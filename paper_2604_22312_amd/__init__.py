@@ -4,7 +4,8 @@ Thin Python binding over the C ABI of ``include/gvr_topk.h`` (library
 ``libgvr_topk.so`` built in-tree by ``paper_2604_22312_amd.build``). This module
 only validates tensors and marshals pointers; every step of the Top-K runs in
 the HIP kernels of ``csrc/gvr_topk.hip``, ``csrc/rope_prior.hip`` and
-``csrc/indexer.hip``. There is no CPU fallback: if the
+``csrc/indexer.hip`` (rotary positions and the 4-bit cache:
+``csrc/rotary.hip``, ``csrc/kv4_cache.hip``, ``csrc/kv4_attention.hip``). There is no CPU fallback: if the
 library is missing, importing the functions raises.
 
 Functions mirror the C entry points:
@@ -26,6 +27,13 @@ Functions mirror the C entry points:
 * ``gvr_indexer_scores(q, w, k, k_scale, ...)`` / ``gvr_indexer_topk(...)`` --
   the FP8 indexer scores, and the indexer followed by gvr_topk
   (``include/gvr_indexer.h``)
+* ``gvr_rope_table(n, ...)`` / ``gvr_rope_rotate(x, positions, table, ...)`` --
+  rotary positions of queries and keys, and of their gradients
+  (``include/gvr_rotary.h``)
+* ``new_kv4_cache`` / ``gvr_kv4_append`` / ``gvr_kv4_read`` /
+  ``gvr_kv4_attention`` -- the paged 4-bit key / value cache: tokens in (keys
+  rotated on the way) and out, and attention over all of a context or over
+  the tokens a Top-K selected (``include/gvr_kv4.h``)
 """
 from .binding import (  # noqa: F401
     GVR_MAX_CANDIDATES,
@@ -58,4 +66,19 @@ from .binding import (  # noqa: F401
     radix_topk_ex_ws,
     status_string,
     version,
+)
+from .kv4 import (  # noqa: F401
+    PreparedOp,
+    gvr_kv4_append,
+    gvr_kv4_attention,
+    gvr_kv4_attention_workspace,
+    gvr_kv4_read,
+    gvr_kv4_record_bytes,
+    gvr_rope_rotate,
+    gvr_rope_table,
+    new_kv4_cache,
+    prepare_gvr_kv4_append,
+    prepare_gvr_kv4_attention,
+    prepare_gvr_kv4_read,
+    prepare_gvr_rope_rotate,
 )

@@ -1,0 +1,77 @@
+// elem_ops.h -- loads and stores of eight consecutive elements of a bfloat16,
+// float16 or float32 tensor as float32 values, for the rotary and the 4-bit
+// cache kernels.
+#ifndef GVR_ELEM_OPS_H
+#define GVR_ELEM_OPS_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#ifndef DEV
+#define DEV __device__ __forceinline__
+#endif
+
+namespace gvr_elem {
+
+typedef float f8 __attribute__((ext_vector_type(8)));
+template <class E> struct Vec8 { typedef E t __attribute__((ext_vector_type(8))); };
+
+// Eight elements at p; wide: p is 16-byte aligned.
+template <bool WIDE, class E>
+DEV f8 load8(const E* p) {
+    if constexpr (WIDE) {
+        return __builtin_convertvector(*reinterpret_cast<const typename Vec8<E>::t*>(p), f8);
+    } else {
+        f8 v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)p[i];
+        return v;
+    }
+}
+
+// Rounded to the nearest, ties to even.
+template <bool WIDE, class E>
+DEV void store8(E* p, f8 v) {
+    if constexpr (WIDE) {
+        *reinterpret_cast<typename Vec8<E>::t*>(p) = __builtin_convertvector(v, typename Vec8<E>::t);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = (E)v[i];
+    }
+}
+
+// Cosine and sine of pair i at a position (row NULL: the position is outside
+// the table, and the pair becomes NaN). NP pairs from an even i of a 16-byte
+// aligned row, or one by one.
+template <int NP, bool WIDE>
+DEV void load_cs(const float* row, int i, float (&c)[NP], float (&s)[NP]) {
+    if (!row) {
+#pragma unroll
+        for (int j = 0; j < NP; ++j) c[j] = s[j] = __builtin_nanf("");
+        return;
+    }
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int j = 0; j < NP; j += 2) {
+            const float4 v = *reinterpret_cast<const float4*>(row + 2 * (i + j));
+            c[j] = v.x, s[j] = v.y, c[j + 1] = v.z, s[j + 1] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < NP; ++j) c[j] = row[2 * (i + j)], s[j] = row[2 * (i + j) + 1];
+    }
+}
+
+// The two halves of a rotation, each product and the sum rounded once.
+DEV float turn_a(float a, float b, float c, float s) {
+#pragma clang fp contract(off)
+    return a * c - b * s;
+}
+DEV float turn_b(float a, float b, float c, float s) {
+#pragma clang fp contract(off)
+    return b * c + a * s;
+}
+
+}  // namespace gvr_elem
+
+#endif  // GVR_ELEM_OPS_H

@@ -1,0 +1,99 @@
+// kv4_plan.h -- the 4-bit cache's record layout, argument checks and the
+// attention's launch plan. Plain C++ with no HIP dependency, so the library
+// and a sanitizer build on the CPU compile the same code.
+#ifndef GVR_KV4_PLAN_H
+#define GVR_KV4_PLAN_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "gvr_kv4.h"
+#include "rotary_plan.h"
+
+namespace gvr_kv4 {
+
+using gvr_rot::kMaxCount;
+
+inline int64_t record_bytes(int kv_heads, int head_dim) {
+    if (kv_heads < 1 || kv_heads > 1024 || !(head_dim == 64 || head_dim == 128 || head_dim == 256)) return -1;
+    return (int64_t)kv_heads * head_dim * 17 / 16;
+}
+
+inline int log2_of(int v) {
+    int s = 0;
+    while ((1 << s) < v) ++s;
+    return s;
+}
+
+// The cache's sizes; its pointer only when slots could be touched.
+inline gvr_status check_cache(const gvr_kv4_cache* c, bool need_data) {
+    if (!c || record_bytes(c->kv_heads, c->head_dim) < 0 || c->reserved != 0) return GVR_ERR_INVALID_ARG;
+    if (c->page_size < 1 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)) || c->pages < 0)
+        return GVR_ERR_INVALID_ARG;
+    if (c->pages > kMaxCount || c->pages * c->page_size > kMaxCount) return GVR_ERR_TOO_LONG;
+    if (need_data && c->pages > 0 && !c->data) return GVR_ERR_INVALID_ARG;
+    if ((uintptr_t)c->data & 15) return GVR_ERR_INVALID_ARG;
+    return GVR_OK;
+}
+
+// The attention's sizes (pointers are the caller's part).
+inline gvr_status check_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_args& a) {
+    if (a.T < 0 || a.sequences < 0 || a.table_width < 0 || a.q_heads < 1 || a.reserved != 0) return GVR_ERR_INVALID_ARG;
+    if (a.q_heads % c.kv_heads || a.q_heads / c.kv_heads > 128) return GVR_ERR_INVALID_ARG;
+    if (!(a.dtype == GVR_BF16 || a.dtype == GVR_F16) || !(a.causal == 0 || a.causal == 1)) return GVR_ERR_INVALID_ARG;
+    if (!(a.scale == a.scale) || a.scale - a.scale != 0.f) return GVR_ERR_INVALID_ARG;   // finite
+    if ((a.q_token_stride | a.q_head_stride) & 7) return GVR_ERR_INVALID_ARG;
+    if (a.selection && a.K < 1) return GVR_ERR_INVALID_ARG;
+    if (a.q_start ? a.max_q < 0 : (a.sequences > 0 && a.T % a.sequences)) return GVR_ERR_INVALID_ARG;
+    if (a.T > kMaxCount || a.table_width > kMaxCount || a.table_width * c.page_size > kMaxCount) return GVR_ERR_TOO_LONG;
+    return GVR_OK;
+}
+
+constexpr int kRows = 16;         // query rows of a wave
+constexpr int kStep = 32;         // tokens of a wave's step
+constexpr int kWaves = 4;         // waves of a workgroup
+constexpr int kMinChunk = 128;    // fewest tokens of a split
+constexpr int kFillWaves = 4096;  // waves that fill the device
+
+struct AttnPlan {
+    int max_q;        // query tokens of a sequence
+    int tiles;        // row tiles of a sequence and KV head
+    int64_t jobs;     // waves
+    int splits;       // of a context or selection
+    int chunk;        // tokens of a split
+    size_t ws_bytes;
+};
+
+inline size_t partial_bytes(int64_t T, int q_heads, int head_dim, int splits) {
+    return splits > 1 ? (size_t)T * q_heads * splits * (head_dim + 2) * 4 : 0;
+}
+
+inline AttnPlan plan_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_args& a, size_t ws_bytes) {
+    AttnPlan p;
+    const int G = a.q_heads / c.kv_heads;
+    p.max_q = a.q_start ? a.max_q : (int)(a.T / a.sequences);
+    if (p.max_q > a.T) p.max_q = (int)a.T;
+    const int64_t tiles = a.selection ? (int64_t)p.max_q * ((G + kRows - 1) / kRows)
+                                      : ((int64_t)p.max_q * G + kRows - 1) / kRows;
+    p.tiles = (int)tiles;
+    const int64_t n = a.selection ? a.K : a.table_width * c.page_size;
+    const int64_t units = (int64_t)a.sequences * tiles * c.kv_heads;
+    int64_t splits = units > 0 ? (kFillWaves + units - 1) / units : 1;
+    const int64_t most = (n + kMinChunk - 1) / kMinChunk;
+    splits = splits > most ? most : splits;
+    splits = splits < 1 ? 1 : splits > 1024 ? 1024 : splits;
+    while (splits > 1 && partial_bytes(a.T, a.q_heads, c.head_dim, (int)splits) > ws_bytes) --splits;
+    int64_t chunk = (n + splits - 1) / splits;
+    chunk = (chunk + kStep - 1) / kStep * kStep;
+    if (chunk < kStep) chunk = kStep;
+    splits = n > 0 ? (n + chunk - 1) / chunk : 1;
+    p.chunk = (int)(chunk > kMaxCount ? kMaxCount / kStep * kStep : chunk);
+    p.splits = (int)splits;
+    p.jobs = units * splits;
+    p.ws_bytes = partial_bytes(a.T, a.q_heads, c.head_dim, p.splits);
+    return p;
+}
+
+}  // namespace gvr_kv4
+
+#endif  // GVR_KV4_PLAN_H

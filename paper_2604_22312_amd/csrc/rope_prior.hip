@@ -42,9 +42,11 @@
 #include "rope_plan.h"
 #pragma clang force_cuda_host_device end
 
-#define DEV __device__ __forceinline__
+#include "yarn.h"
 
 namespace {
+
+using namespace gvr_yarn;
 
 using gvr_rope::kGLanes;
 using gvr_rope::kGPer;
@@ -53,7 +55,6 @@ using gvr_rope::kLinBins;
 using gvr_rope::kMaxN;
 using gvr_rope::lin_bin;
 
-constexpr int kMaxPairs = 256;               // d <= 512
 constexpr int kSBlock = 1024;                // threads of the select workgroup
 constexpr int kSWaves = kSBlock / 64;
 constexpr int kSelBins = 2048;               // widest digit: 11 bits
@@ -63,26 +64,6 @@ constexpr int kEmitPer = 4;                  // consecutive elements per thread 
 
 __constant__ int kDigitShift[kDigits] = {53, 42, 31, 20, 10, 0};
 __constant__ int kDigitBits[kDigits] = {11, 11, 11, 11, 10, 10};
-
-struct RopeArgs {
-    int d;
-    int orig_ctx;
-    double base, scale, beta_fast, beta_slow;
-};
-
-// theta'_i of one rotary pair (YaRN ramp over the pair index).
-DEV double yarn_angle(int i, const RopeArgs& a) {
-#pragma clang fp contract(off)
-    const double two_pi = 6.283185307179586;
-    const double ln_base = log(a.base);
-    const double x_fast = a.d * log(a.orig_ctx / (two_pi * a.beta_fast)) / (2.0 * ln_base);
-    const double x_slow = a.d * log(a.orig_ctx / (two_pi * a.beta_slow)) / (2.0 * ln_base);
-    const double lo = fmax(floor(x_fast), 0.0);
-    const double hi = fmin(ceil(x_slow), (double)(a.d - 1));
-    const double theta = pow(a.base, -2.0 * i / a.d);
-    const double gamma = fmin(fmax((i - lo) / fmax(hi - lo, 1e-3), 0.0), 1.0);
-    return theta * (1.0 - gamma) + (theta / a.scale) * gamma;
-}
 
 template <int LANES>
 __global__ __launch_bounds__(kGPer * LANES) void rope_g_kernel(int64_t n, RopeArgs a, double* __restrict__ g,
@@ -425,27 +406,6 @@ __global__ __launch_bounds__(kSBlock) void prior_select_kernel(const double* __r
         carry_eq += tot_eq;
         carry_sel += tot_sel;
     }
-}
-
-bool finite_pos(double v) { return isfinite(v) && v > 0.0; }
-
-gvr_status read_params(const gvr_rope_params* p, RopeArgs* a) {
-    gvr_rope_params d;
-    if (!p) {
-        gvr_rope_params_default(&d);
-        p = &d;
-    }
-    if (p->d_rope < 2 || p->d_rope > 2 * kMaxPairs || (p->d_rope & 1)) return GVR_ERR_INVALID_ARG;
-    if (p->orig_ctx < 1) return GVR_ERR_INVALID_ARG;
-    if (!isfinite(p->base) || p->base <= 1.0) return GVR_ERR_INVALID_ARG;
-    if (!finite_pos(p->scale) || !finite_pos(p->beta_fast) || !finite_pos(p->beta_slow)) return GVR_ERR_INVALID_ARG;
-    a->d = p->d_rope;
-    a->orig_ctx = p->orig_ctx;
-    a->base = p->base;
-    a->scale = p->scale;
-    a->beta_fast = p->beta_fast;
-    a->beta_slow = p->beta_slow;
-    return GVR_OK;
 }
 
 gvr_status launch_g(int64_t n, const RopeArgs& a, double* g, double* theta, void* stream) {
