@@ -67,7 +67,7 @@ gvr_status gvr_kv4_append(const gvr_kv4_cache* cache, const gvr_heads* k, const 
 
 /* Read T tokens back: k and v [T][kv_heads][head_dim] of type `dtype` receive
  * the values that the records at slots [T] stand for (exact in bfloat16 and
- * float32, rounded in float16); zeros for a slot outside the cache. Either of
+ * float32, where only a code of 2^128 overflows; rounded in float16); zeros for a slot outside the cache. Either of
  * k and v may be NULL. Errors as gvr_kv4_append. */
 gvr_status gvr_kv4_read(const gvr_kv4_cache* cache, const gvr_heads* k, const gvr_heads* v, int32_t dtype, int64_t T,
                         const int64_t* slots, void* stream);
