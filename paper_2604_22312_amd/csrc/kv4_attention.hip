@@ -2,22 +2,34 @@
 // include/gvr_kv4.h.
 //
 // One wave serves 16 query rows (the query heads of one KV head, of one or
-// more query tokens of a sequence) over a chunk of the context, 32 tokens a
-// step, on the 16-bit matrix cores:
+// more query tokens of a sequence) over steps of 32 tokens:
 //     S^T [tokens][rows] = K Q^T,   P = exp2(S - m),   O^T [dims][rows] += V^T P^T
 // Lane l holds column l % 16 (its query row) and quarter l / 16. The order of
-// the dimensions inside the first product and of the tokens inside the second
-// is free, and is chosen so that nothing moves between lanes:
-//   - K: a lane takes D / 4 consecutive dimensions of one token per 16, one
-//     load of D / 8 bytes of codes that share one scale (D = 256: two);
+// the tokens inside the second product is free, and is chosen so that nothing
+// moves between lanes:
+//   - K goes into gfx950's scaled matrix instruction as it is stored: a lane
+//     takes 32 dimensions (16 bytes of codes) of one token per 16, and their
+//     scale byte is the instruction's block scale. The queries are its 8-bit
+//     operand: each is the sum of two E4M3 numbers (three for float16) with
+//     power-of-two scales 2^-4 apart, which holds a bfloat16 exactly down to
+//     2^-14 of its block's largest magnitude (an error of at most 2^-21 of it
+//     below). Against unpacking K for the 16-bit instruction this costs the
+//     same matrix time and 32 vector instructions a step less;
 //   - the scores that come out sit in the lane that feeds them, as weights, to
 //     the second product: tokens 4 q + i of both halves of the step;
 //   - V: for those tokens a lane takes D / 16 consecutive dimensions, and the
-//     n-th of them goes to the n-th matrix step.
-// gfx950's conversion turns two codes and their scale into two 16-bit floats
-// in one instruction; the values of two tokens are then paired by byte
-// permutes. Running maximum and sum are float32 per row; chunks of one
-// context are joined by a second kernel from float32 partial results.
+//     n-th of them goes to the n-th matrix step. One instruction turns two
+//     codes and their scale into two 16-bit floats; the values of two tokens
+//     are then paired by byte permutes. (The scales of V lie along the
+//     dimensions, across the product's sum, so V cannot go in as stored.)
+// Sum and maximum are float32 per row. The maximum that the weights refer to
+// moves only when a score passes it by 8 (in the exponent of two), so most
+// steps neither exchange it between lanes nor rescale O; weights are at most
+// 2^8 then.
+//
+// A workgroup is `hw` KV heads x `tw` waves that take turns at the steps of
+// one chunk of a context; its waves are joined in LDS, chunks of a context by
+// a second kernel from float32 partial results.
 
 #include <hip/hip_runtime.h>
 
@@ -32,13 +44,17 @@ namespace {
 
 using gvr_kv4::kRows;
 using gvr_kv4::kStep;
-using gvr_kv4::kWaves;
+using gvr_kv4::kMaxWaves;
+using gvr_kv4::kSlots;
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef int v8i __attribute__((ext_vector_type(8)));
 template <class E> struct Vec { typedef E x8 __attribute__((ext_vector_type(8))); typedef E x2 __attribute__((ext_vector_type(2))); };
 
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int kBufWord3 = 0x00020000;    // raw buffer resource: 32-bit data format, no swizzle
 constexpr float kLn2 = 0.693147180559945309417f;
 
 struct AttnParams {
@@ -53,8 +69,10 @@ struct AttnParams {
     const int32_t* q_start;
     const int32_t* selection;
     int64_t qt, qh;   // query strides
-    int64_t table_width, pages, record, T, jobs;
+    int64_t table_width, record, T, jobs;
     int32_t page_shift, kv_heads, q_heads, group, sequences, uniform_q, max_q, tiles, splits, chunk, K, causal;
+    int32_t pages;
+    int32_t hw_shift, tw_shift;   // log2 of a workgroup's KV heads, and of the waves that share a head's steps
     float scale2;     // scale * log2(e)
 };
 
@@ -62,7 +80,7 @@ struct AttnParams {
 template <class E>
 DEV uint32_t unpack(uint32_t w, float scale, int sel) {
     typename Vec<E>::x2 v;
-    if constexpr (sizeof(E) == 2 && __is_same(E, __bf16)) {
+    if constexpr (__is_same(E, __bf16)) {
         v = sel == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)
             : sel == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)
             : sel == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)
@@ -83,15 +101,28 @@ DEV v4f mfma(v4u a, v4u b, v4f c) {
     else
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
 }
+// 16 tokens x 128 dimensions in 4 bits times 128 dimensions x 16 rows in 8 bits.
+constexpr int kFp8 = 0, kFp4 = 4;
+DEV v4f mfma_mx(v4u a, uint32_t sa, v8i b, uint32_t sb, v4f c) {
+    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b, c, kFp4, kFp8, 0, (int)sa, 0, (int)sb);
+}
 template <class E>
 DEV uint32_t pack2(float a, float b) {
     typename Vec<E>::x2 v;
     v[0] = (E)a, v[1] = (E)b;
     return __builtin_bit_cast(uint32_t, v);
 }
+// The largest of three (without the compiler's quieting of each operand: what
+// a NaN gives does not matter, its weight is NaN in any case).
+DEV float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 DEV float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// NB bytes of codes at p as dwords (4-byte aligned; two bytes: 2-byte aligned).
+// NB bytes of codes as dwords (records are 4-byte aligned, runs of 2 bytes 2-byte).
 template <int NB>
 struct Codes {
     uint32_t w[NB / 4 ? NB / 4 : 1];
@@ -101,21 +132,109 @@ DEV Codes<NB> load_codes(const uint8_t* p) {
     Codes<NB> c;
     if constexpr (NB == 2) {
         c.w[0] = *reinterpret_cast<const uint16_t*>(p);
+    } else if constexpr (NB == 4) {
+        c.w[0] = *reinterpret_cast<const uint32_t*>(p);
     } else {
-        typedef uint32_t vec __attribute__((ext_vector_type(NB / 4 > 4 ? 4 : NB / 4), aligned(4)));
+        typedef uint32_t vec __attribute__((ext_vector_type(NB / 4), aligned(4)));
+        const vec v = *reinterpret_cast<const vec*>(p);
 #pragma unroll
-        for (int i = 0; i < NB / 4; i += 4) {
-            const vec v = *reinterpret_cast<const vec*>(p + 4 * i);
+        for (int j = 0; j < NB / 4; ++j) c.w[j] = v[j];
+    }
+    return c;
+}
+DEV v4u load16(const uint8_t* p) {
+    typedef uint32_t vec __attribute__((ext_vector_type(4), aligned(4)));
+    return *reinterpret_cast<const vec*>(p);
+}
+
+// A query row as 8-bit terms for the scaled product: T terms per run of 128
+// dimensions (D = 64: the run holds the dimensions twice, for two terms).
+// Byte i of a lane's half-run r is dimension 64 r + 16 quarter + i; a lane's
+// scale byte is that of the dimensions 32 quarter ..
+template <class E, int D>
+struct Query {
+    static constexpr int kTerms = __is_same(E, __bf16) ? 2 : 3;
+    static constexpr int kRuns = D == 64 ? (kTerms + 1) / 2 : D / 128;
+    static constexpr int kPer = D == 64 ? 1 : kTerms;   // products per run
+    v8i b[kRuns][kPer];
+    uint32_t scale[kRuns][kPer];
+};
+
+// Sixteen elements as four dwords of E4M3, and what is left of them times 16.
+DEV void split16(float (&x)[16], v8i& out, int at) {
 #pragma unroll
-            for (int j = 0; j < (NB / 4 > 4 ? 4 : NB / 4); ++j) {
-                if constexpr (NB == 4)
-                    c.w[0] = v[0];
-                else
-                    c.w[i + j] = v[j];
+    for (int i = 0; i < 4; ++i) {
+        int w = 0;
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i], x[4 * i + 1], w, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2], x[4 * i + 3], w, true);
+        out[at + i] = w;
+        x[4 * i] = 16.f * (x[4 * i] - __builtin_amdgcn_cvt_f32_fp8(w, 0));
+        x[4 * i + 1] = 16.f * (x[4 * i + 1] - __builtin_amdgcn_cvt_f32_fp8(w, 1));
+        x[4 * i + 2] = 16.f * (x[4 * i + 2] - __builtin_amdgcn_cvt_f32_fp8(w, 2));
+        x[4 * i + 3] = 16.f * (x[4 * i + 3] - __builtin_amdgcn_cvt_f32_fp8(w, 3));
+    }
+}
+
+// q: the row's D elements (NULL: zeros), times sign. Lanes of one row must
+// all be active. Not finite: the block's scale is NaN.
+template <class E, int D>
+DEV Query<E, D> load_query(const E* q, float sign, int lane) {
+    typedef typename Vec<E>::x8 x8;
+    const int col = lane & 15, quarter = lane >> 4;
+    Query<E, D> r;
+    // scale of the 32 dimensions from 32 quarter (+ 128 per run): largest magnitude in [2^7, 2^8)
+    constexpr int kBlocks = D == 256 ? 2 : 1;
+    uint32_t byte[kBlocks];
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) {
+        uint32_t m = 0;
+        if (q) {
+            const E* p = q + 128 * c + 32 * (D == 64 ? quarter & 1 : quarter);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const x8 v = *reinterpret_cast<const x8*>(p + 8 * i);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint((float)v[j]) & 0x7FFFFFFFu);
+            }
+        }
+        const int e = (int)(m >> 23);
+        byte[c] = e == 255 ? 255u : (uint32_t)max(e - 7, 16);   // 16: room for the lower terms
+    }
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) {
+        float x[2][16];   // half-runs
+#pragma unroll
+        for (int h = 0; h < (D == 64 ? 1 : 2); ++h) {
+            const uint32_t b = (uint32_t)__shfl((int)byte[c], col + 16 * (2 * h + (quarter >> 1)), 64);
+            const float inv = b == 255 ? 0.f : __uint_as_float((254u - b) << 23) * sign;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                x8 v = {};
+                if (q) v = *reinterpret_cast<const x8*>(q + 128 * c + 64 * h + 16 * quarter + 8 * i);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[h][8 * i + j] = b == 255 ? 0.f : (float)v[j] * inv;
+            }
+        }
+        if constexpr (D == 64) {
+            // terms 0 and 1 share a run, term 2 has the lower half of another
+#pragma unroll
+            for (int t = 0; t < r.kTerms; ++t) split16(x[0], r.b[t / 2][0], 4 * (t & 1));
+            r.scale[0][0] = byte[0] == 255 ? 255u : byte[0] - (quarter >= 2 ? 4u : 0u);
+            if constexpr (r.kTerms == 3) {
+#pragma unroll
+                for (int i = 4; i < 8; ++i) r.b[1][0][i] = 0;
+                r.scale[1][0] = byte[0] == 255 ? 255u : byte[0] - 8u;
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < r.kTerms; ++t) {
+                split16(x[0], r.b[c][t], 0);
+                split16(x[1], r.b[c][t], 4);
+                r.scale[c][t] = byte[c] == 255 ? 255u : byte[c] - 4u * t;
             }
         }
     }
-    return c;
+    return r;
 }
 
 // Sequence b's query tokens: rows q0 .. q0 + nq - 1 of q, the first `shown` served.
@@ -136,203 +255,257 @@ DEV Rows rows_of(const AttnParams& p, int b) {
     return r;
 }
 
-template <class E, int D, bool SEL>
-__global__ __launch_bounds__(kWaves * 64) void few_rows_kernel(AttnParams p) {
-    constexpr int KS = D / 32;        // matrix steps of the first product
-    constexpr int NT = D / 16;        // dimensions of V per lane = matrix steps of the second
+// What a wave loads for a step of 32 tokens.
+template <int D>
+struct Step {
+    static constexpr int kRuns = D == 256 ? 2 : 1;
+    static constexpr int kVWords = D == 256 ? 2 : 1;
+    v4u k[2][kRuns];          // codes of the token of this lane's column
+    uint32_t ks[2][kRuns];    // their scale bytes
+    Codes<D / 32> v[8];       // codes of the lane's eight tokens
+    uint32_t vs[8];           // their scale bytes
+    uint32_t there;           // bit n: token n exists
+    int t0;
+};
+
+// GATHER: the tokens' slots come from LDS (a selection, or pages of fewer than
+// 16 tokens); else from two page numbers per step.
+template <class E, int D, bool GATHER>
+__global__ __launch_bounds__(kMaxWaves * 64, 2) void few_rows_kernel(AttnParams p) {
+    constexpr int NT = D / 16;        // dimensions of V per lane = matrix steps of the second product
+    typedef Query<E, D> Q;
+    extern __shared__ uint8_t lds[];
     const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
-    // wave-uniform: head fastest (neighbouring waves read neighbouring parts of the records)
-    int64_t job = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (job >= p.jobs) return;
-    const int h = (int)(job % p.kv_heads);
-    job /= p.kv_heads;
-    const int tile = (int)(job % p.tiles);
-    job /= p.tiles;
-    const int split = (int)(job % p.splits);
-    const int b = (int)(job / p.splits);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tg = wave >> p.hw_shift;                    // turn of this wave at the steps
+    uint32_t job = blockIdx.x;
+    const int groups = p.kv_heads >> p.hw_shift;
+    const int h = (int)(job % (uint32_t)groups << p.hw_shift) + (wave & ((1 << p.hw_shift) - 1));
+    job /= (uint32_t)groups;
+    const int tile = (int)(job % (uint32_t)p.tiles);
+    job /= (uint32_t)p.tiles;
+    const int split = (int)(job % (uint32_t)p.splits);
+    const int b = (int)(job / (uint32_t)p.splits);
 
     const Rows rows = rows_of(p, b);
     const int64_t q0 = rows.q0, nq = rows.nq;
     const int shown = rows.shown;
     if (shown <= 0) return;
     const int64_t held = p.table_width << p.page_shift;
-    const int ctx = (int)min((int64_t)max(p.ctx_len[b], 0), held);
+    const int ctx = p.pages > 0 ? (int)min((int64_t)max(p.ctx_len[b], 0), held) : 0;
+    const bool sel = GATHER && p.selection;
 
-    // this lane's query row
-    int qi, qg;   // query token of the sequence, head of the group
+    // this lane's query row; tokens [0, end) of the context or selection concern the tile
+    int qi, qg, end, sel_last = 0;
     bool live;
-    if constexpr (SEL) {
+    const int32_t* list = nullptr;
+    if (sel) {
         const int per = (p.group + kRows - 1) / kRows;
         qi = tile / per;
         qg = (tile - qi * per) * kRows + col;
-        live = qi < shown && qg < p.group;
         if (qi >= shown) return;
+        live = qg < p.group;
+        end = p.pages > 0 ? p.K : 0;
+        list = p.selection + (q0 + qi) * p.K;
+        sel_last = p.causal ? (int)(ctx - nq + qi) : ctx - 1;
     } else {
         const int r = tile * kRows + col;
         qi = r / p.group;
         qg = r - qi * p.group;
         live = qi < shown;
         if ((tile * kRows) / p.group >= shown) return;
-    }
-    const int64_t row = q0 + qi;
-    const int hq = h * p.group + qg;
-    // last visible token of this row; of the wave's rows, the last row's is the largest
-    const int last = live ? (p.causal ? (int)(ctx - nq + qi) : ctx - 1) : -1;
-    int end;
-    if constexpr (SEL) {
-        end = p.K;
-    } else {
         const int qi_last = min((tile * kRows + kRows - 1) / p.group, shown - 1);
         end = (int)max((int64_t)0, p.causal ? ctx - nq + qi_last + 1 : (int64_t)ctx);
     }
+    const int64_t row = q0 + qi;
+    const int hq = h * p.group + qg;
+    // last token that this lane's row sees, and the last that all of the tile's rows see
+    const int last = !live ? -1 : sel ? 0x7FFFFFFF : p.causal ? (int)(ctx - nq + qi) : ctx - 1;
+    const int all_last = sel ? 0x7FFFFFFF
+                             : (int)max((int64_t)-1, p.causal ? ctx - nq + (tile * kRows) / p.group : (int64_t)ctx - 1);
     const int64_t lo = (int64_t)split * p.chunk;
     const int begin = (int)min(lo, (int64_t)end), stop = (int)min(lo + p.chunk, (int64_t)end);
 
-    // queries: for matrix step s the lane holds dimensions quarter * D / 4 + 8 s ..
-    v4u qf[KS];
-    {
-        const uint16_t* qp = static_cast<const uint16_t*>(p.q) + (live ? row * p.qt + hq * p.qh : 0) + quarter * (D / 4);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const v4u v = *reinterpret_cast<const v4u*>(qp + 8 * s);
-            qf[s] = live ? v : v4u{0, 0, 0, 0};
-        }
-    }
-    const int64_t k_off = (int64_t)h * (D / 2) + quarter * (D / 8);
-    const int64_t v_off = (int64_t)(p.kv_heads + h) * (D / 2) + col * (D / 32);
-    const int64_t ks_off = (int64_t)p.kv_heads * D + h * (D / 32) + quarter * (D / 4) / 32;
-    const int64_t vs_off = (int64_t)p.kv_heads * D + (p.kv_heads + h) * (D / 32) + col * (D / 16) / 32;
+    const float scale2 = fabsf(p.scale2);
+    const Q q = load_query<E, D>(live ? static_cast<const E*>(p.q) + row * p.qt + hq * p.qh : nullptr,
+                                 p.scale2 < 0.f ? -1.f : 1.f, lane);
+    const uint32_t record = (uint32_t)p.record;
+    const uint32_t k_off = h * (D / 2) + 16 * (D == 64 ? quarter & 1 : quarter);
+    const uint32_t v_off = (p.kv_heads + h) * (D / 2) + col * (D / 32);
+    const uint32_t ks_off = p.kv_heads * D + h * (D / 32) + (D == 64 ? quarter & 1 : quarter);
+    const uint32_t vs_off = p.kv_heads * D + (p.kv_heads + h) * (D / 32) + col * (D / 16) / 32;
     const int32_t* table = p.block_table + (int64_t)b * p.table_width;
-    const int32_t* list = SEL ? p.selection + row * p.K : nullptr;
-    const int sel_last = SEL ? (p.causal ? (int)(ctx - nq + qi) : ctx - 1) : 0;   // the same for the wave's rows
     const int page_mask = (1 << p.page_shift) - 1;
+    const int stride = kStep << p.tw_shift;
 
-    // last token that the wave's first row sees (all rows see what it sees)
-    const int64_t first_last = p.causal ? ctx - nq + (tile * kRows) / p.group : (int64_t)ctx - 1;
-
-    float m = -INFINITY, sum = 0.f;
+    float m = -INFINITY, limit = -INFINITY, base = 0.f, sum = 0.f;
+    // maximum (of unscaled scores) that the weights refer to, the score that moves it, maximum * scale2
     v4f o[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) o[n] = v4f{0.f, 0.f, 0.f, 0.f};
 
-    for (int t0 = begin; t0 < stop; t0 += kStep) {
-        // slots of tokens t0 + lane % 32 (-1: not there)
-        int slot = -1;
-        {
-            const int n = t0 + (lane & 31);
-            int tok = n;
-            bool there = n < stop;
-            if constexpr (SEL) {
-                if (there) tok = list[n];
-                there = there && tok >= 0 && tok <= sel_last;
-            }
-            if (there) {
-                const int page = table[tok >> p.page_shift];
-                if (page >= 0 && page < p.pages) slot = (page << p.page_shift) + (tok & page_mask);
-            }
-        }
-        const uint32_t there = (uint32_t)__ballot(slot >= 0);
-        if (there == 0) continue;
-        slot = max(slot, 0);
-        v4f sc[2];
+    // Slots of a step's two runs of 16 tokens from page numbers (scalar). A
+    // run that is not there, and a run's tokens past its end, read records
+    // that are in the cache (a page of 16 or more holds the whole run).
+    // The loads go through a buffer resource over the run: a lane's offset is
+    // a constant, and what a scalar adds costs no vector instruction.
+    const int ko = (int)(col * record + k_off), kso = (int)(col * record + ks_off);
+    const int vo = (int)(4 * quarter * record + v_off), vso = (int)(4 * quarter * record + vs_off);
+    auto fetch_dense = [&](int t0, Step<D>& d) {
+        d.t0 = t0;
+        d.there = 0;
+        __amdgpu_buffer_rsrc_t run[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const uint8_t* rec = p.cache + (int64_t)__shfl(slot, 16 * t + col, 64) * p.record;
-            const Codes<D / 8> kc = load_codes<D / 8>(rec + k_off);
-            const float s0 = scale_of(rec[ks_off]);
-            const float s1 = D == 256 ? scale_of(rec[ks_off + 1]) : s0;
-            v4f acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const float ss = D == 256 && s >= KS / 2 ? s1 : s0;
-                const v4u a = {unpack<E>(kc.w[s], ss, 0), unpack<E>(kc.w[s], ss, 1), unpack<E>(kc.w[s], ss, 2),
-                               unpack<E>(kc.w[s], ss, 3)};
-                acc = mfma<E>(a, qf[s], acc);
-            }
-            sc[t] = acc;
+            const int tok = t0 + 16 * t;
+            const int n = min(stop - tok, 16);   // tokens of this run
+            const int page = n > 0 ? table[tok >> p.page_shift] : -1;
+            const bool ok = (uint32_t)page < (uint32_t)p.pages;
+            if (ok) d.there |= (n >= 16 ? 0xFFFFu : (1u << n) - 1u) << (16 * t);
+            const uint64_t slot = ok ? (uint32_t)((page << p.page_shift) + (tok & page_mask)) : 0u;
+            run[t] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p.cache) + slot * record, (short)0,
+                                                       (int)(16 * record), kBufWord3);
         }
-        // mask, running maximum
-        float top = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int n = 16 * t + 4 * quarter + i;
-                const bool see = ((there >> n) & 1) && (SEL ? live : t0 + n <= last);
-                sc[t][i] = see ? sc[t][i] * p.scale2 : -INFINITY;
-                top = fmaxf(top, sc[t][i]);
+            for (int c = 0; c < Step<D>::kRuns; ++c) {
+                d.k[t][c] = __builtin_amdgcn_raw_buffer_load_b128(run[t], ko + 64 * c, 0, 0);
+                d.ks[t][c] = __builtin_amdgcn_raw_buffer_load_b8(run[t], kso + 4 * c, 0, 0);
             }
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float m_new = fmaxf(m, top);
-        const float base = m_new == -INFINITY ? 0.f : m_new;   // nothing seen so far: all weights are zero
-        const float keep = exp2f(m - base);
-        m = m_new;
-        sum *= keep;
-        v4u pf;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            float w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = exp2f(sc[t][i] - base);
-                sum += w[i];
-            }
-            pf[2 * t] = pack2<E>(w[0], w[1]);
-            pf[2 * t + 1] = pack2<E>(w[2], w[3]);
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) o[n] *= keep;
-        // values: a masked token's weight is zero, and its codes are taken as
-        // zero too (a NaN block times zero would not be)
-        uint32_t vw[8][D == 256 ? 2 : 1];
-        float vs[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int n = 16 * (j >> 2) + 4 * quarter + (j & 3);
-            const uint8_t* rec = p.cache + (int64_t)__shfl(slot, n, 64) * p.record;
-            const Codes<D / 32> c = load_codes<D / 32>(rec + v_off);
-            const bool see = (there >> n) & 1;
-#pragma unroll
-            for (int i = 0; i < (D == 256 ? 2 : 1); ++i) vw[j][i] = see ? c.w[i] : 0u;
-            vs[j] = see ? scale_of(rec[vs_off]) : 1.f;
+            const int at = (j & 3) * (int)record;
+            if constexpr (D == 64) {
+                d.v[j].w[0] = __builtin_amdgcn_raw_buffer_load_b16(run[j >> 2], vo, at, 0);
+            } else if constexpr (D == 128) {
+                d.v[j].w[0] = __builtin_amdgcn_raw_buffer_load_b32(run[j >> 2], vo, at, 0);
+            } else {
+                const v2u v = __builtin_amdgcn_raw_buffer_load_b64(run[j >> 2], vo, at, 0);
+                d.v[j].w[0] = v[0], d.v[j].w[1] = v[1];
+            }
+            d.vs[j] = __builtin_amdgcn_raw_buffer_load_b8(run[j >> 2], vso, at, 0);
         }
-        // Where the wave's rows see different tokens, a NaN value block must
-        // not meet the zero weight of a row that does not see it: it is taken
-        // out, and the rows that see it are found by a product of indicators.
-        if (!SEL && t0 + kStep - 1 > first_last) {
+    };
+    // From record offsets in LDS (-1: not there).
+    const int64_t* offs = reinterpret_cast<const int64_t*>(lds);
+    const uint8_t *const kp = p.cache + k_off, *const ksp = p.cache + ks_off, *const vp = p.cache + v_off,
+                         *const vsp = p.cache + vs_off;
+    auto fetch_gather = [&](int t0, int t_lds, bool in, Step<D>& d) {
+        d.t0 = t0;
+        t_lds = in ? t_lds : 0;
+        d.there = in ? (uint32_t)__ballot(offs[t_lds + (lane & 31)] >= 0) : 0u;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int64_t at = max(offs[t_lds + 16 * t + col], (int64_t)0);
+#pragma unroll
+            for (int c = 0; c < Step<D>::kRuns; ++c) {
+                d.k[t][c] = load16(kp + at + 64 * c);
+                d.ks[t][c] = ksp[at + 4 * c];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t at = max(offs[t_lds + 16 * (j >> 2) + 4 * quarter + (j & 3)], (int64_t)0);
+            d.v[j] = load_codes<D / 32>(vp + at);
+            d.vs[j] = vsp[at];
+        }
+    };
+
+    auto use = [&](Step<D>& d) {
+        if (d.there == 0) return;
+        v4f sc[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            v4f acc = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (D == 64) {
+#pragma unroll
+                for (int r = 0; r < Q::kRuns; ++r) acc = mfma_mx(d.k[t][0], d.ks[t][0], q.b[r][0], q.scale[r][0], acc);
+            } else {
+#pragma unroll
+                for (int c = 0; c < Q::kRuns; ++c)
+#pragma unroll
+                    for (int u = Q::kPer - 1; u >= 0; --u)
+                        acc = mfma_mx(d.k[t][c], d.ks[t][c], q.b[c][u], q.scale[c][u], acc);
+            }
+            sc[t] = acc;
+        }
+        const bool full = d.there == 0xFFFFFFFFu && d.t0 + kStep - 1 <= all_last;   // wave-uniform
+        uint32_t seen = 0xFFu;   // bit 4 t + i: this row sees token 16 t + 4 quarter + i
+        if (!full) {
+            seen = 0;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int n = 16 * t + 4 * quarter + i;
+                    const bool see = ((d.there >> n) & 1) && d.t0 + n <= last;
+                    seen |= see ? 1u << (4 * t + i) : 0u;
+                    if (!see) sc[t][i] = -INFINITY;
+                }
+        }
+        float top = max3(max3(max3(sc[0][0], sc[0][1], sc[0][2]), sc[0][3], sc[1][0]), sc[1][1],
+                         fmaxf(sc[1][2], sc[1][3]));
+        if (__any(top > limit)) {
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float m_new = fmaxf(m, top);
+            // (nothing seen so far: sum and O are zero)
+            const float keep = m_new == m || m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m_new) * scale2);
+            m = m_new;
+            base = m == -INFINITY ? 0.f : m * scale2;
+            limit = scale2 > 0.f ? m + 8.f / scale2 : m;
+            sum *= keep;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[n] *= keep;
+        }
+        float w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j >> 2][j & 3], scale2, -base));
+        float vs[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) vs[j] = scale_of(d.vs[j]);
+        if (!full) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = (seen >> j) & 1 ? w[j] : 0.f;
+            // A masked token's weight is zero, but a NaN block times zero is
+            // not. Tokens that are not there are taken as zeros. Where the
+            // rows see different tokens, a NaN block is taken out, and the
+            // rows that see it are found by a product of indicators.
             uint32_t bad = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) bad |= __float_as_uint(vs[j]) == 0x7F800000u ? 1u << j : 0u;
-            if (__ballot(bad != 0)) {
-                v4u ind, seen;
+            for (int j = 0; j < 8; ++j) {
+                const bool here = (d.there >> (16 * (j >> 2) + 4 * quarter + (j & 3))) & 1;
+                const bool nan = __float_as_uint(vs[j]) == 0x7F800000u;
+                bad |= here && nan ? 1u << j : 0u;
+                if (!here || nan) {
+                    vs[j] = 0.f;
+                    d.v[j] = Codes<D / 32>{};
+                }
+            }
+            if (__any(bad != 0)) {
+                v4u ind, see;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     ind[j] = pack2<E>((bad >> (2 * j)) & 1 ? 1.f : 0.f, (bad >> (2 * j + 1)) & 1 ? 1.f : 0.f);
-                    seen[j] = pack2<E>(sc[j >> 1][2 * (j & 1)] > -INFINITY || sc[j >> 1][2 * (j & 1)] != sc[j >> 1][2 * (j & 1)] ? 1.f : 0.f,
-                                       sc[j >> 1][2 * (j & 1) + 1] > -INFINITY || sc[j >> 1][2 * (j & 1) + 1] != sc[j >> 1][2 * (j & 1) + 1] ? 1.f : 0.f);
+                    see[j] = pack2<E>((seen >> (2 * j)) & 1 ? 1.f : 0.f, (seen >> (2 * j + 1)) & 1 ? 1.f : 0.f);
                 }
-                const v4f hits = mfma<E>(ind, seen, v4f{0.f, 0.f, 0.f, 0.f});
+                const v4f hits = mfma<E>(ind, see, v4f{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float nan = hits[i] > 0.f ? __builtin_nanf("") : 0.f;
 #pragma unroll
                     for (int n = 0; n < NT; ++n) o[n][i] += nan;
                 }
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if ((bad >> j) & 1) {
-                        vs[j] = 1.f;
-                        vw[j][0] = 0u;
-                        if constexpr (D == 256) vw[j][1] = 0u;
-                    }
             }
         }
+        sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        const v4u pf = {pack2<E>(w[0], w[1]), pack2<E>(w[2], w[3]), pack2<E>(w[4], w[5]), pack2<E>(w[6], w[7])};
 #pragma unroll
         for (int n = 0; n < NT; n += 2) {
             uint32_t u[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = unpack<E>(vw[j][n / 8], vs[j], (n % 8) / 2);
+            for (int j = 0; j < 8; ++j) u[j] = unpack<E>(d.v[j].w[n / 8], vs[j], (n % 8) / 2);
             v4u a0, a1;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -342,18 +515,84 @@ __global__ __launch_bounds__(kWaves * 64) void few_rows_kernel(AttnParams p) {
             o[n] = mfma<E>(a0, pf, o[n]);
             o[n + 1] = mfma<E>(a1, pf, o[n + 1]);
         }
+    };
+
+    // The loads of the next step go out before a step is used.
+    if constexpr (!GATHER) {
+        int t0 = begin + kStep * tg;
+        if (t0 < stop) {
+            Step<D> d[2];
+            fetch_dense(t0, d[0]);
+            for (; t0 < stop; t0 += 2 * stride) {
+                fetch_dense(t0 + stride, d[1]);
+                use(d[0]);
+                fetch_dense(t0 + 2 * stride, d[0]);
+                use(d[1]);
+            }
+        }
+    } else {
+        for (int piece = begin; piece < stop; piece += kSlots) {
+            const int fill = min(stop - piece, kSlots);
+            __syncthreads();   // the waves are through with the last piece
+            for (int i = threadIdx.x; i < (fill + kStep - 1) / kStep * kStep; i += blockDim.x) {
+                int64_t at = -1;
+                if (i < fill) {
+                    const int tok = sel ? list[piece + i] : piece + i;
+                    if (tok >= 0 && (!sel || tok <= sel_last)) {
+                        const int page = table[tok >> p.page_shift];
+                        if ((uint32_t)page < (uint32_t)p.pages) at = (((int64_t)page << p.page_shift) + (tok & page_mask)) * record;
+                    }
+                }
+                reinterpret_cast<int64_t*>(lds)[i] = at;
+            }
+            __syncthreads();
+            int t = kStep * tg;
+            if (t < fill) {
+                Step<D> d[2];
+                fetch_gather(piece + t, t, true, d[0]);
+                for (; t < fill; t += 2 * stride) {
+                    fetch_gather(piece + t + stride, t + stride, t + stride < fill, d[1]);
+                    use(d[0]);
+                    fetch_gather(piece + t + 2 * stride, t + 2 * stride, t + 2 * stride < fill, d[0]);
+                    use(d[1]);
+                }
+            }
+        }
     }
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
-    if (!live) return;
+
+    // Join the waves of a head: half of them hand theirs to the other half.
+    for (int half = (1 << p.tw_shift) >> 1; half > 0; half >>= 1) {
+        const int places = half << p.hw_shift;   // of waves in LDS
+        const int place = (tg & (half - 1)) << p.hw_shift | (wave & ((1 << p.hw_shift) - 1));
+        v4f* lo4 = reinterpret_cast<v4f*>(lds) + (place * NT) * 64 + lane;
+        float2* lml = reinterpret_cast<float2*>(lds + (size_t)places * NT * 1024) + place * 64 + lane;
+        __syncthreads();
+        if (tg >= half && tg < 2 * half) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) lo4[n * 64] = o[n];
+            *lml = float2{m, sum};
+        }
+        __syncthreads();
+        if (tg < half) {
+            const float2 other = *lml;
+            const float m_new = fmaxf(m, other.x);
+            const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * scale2);
+            const float theirs = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((other.x - m_new) * scale2);
+            sum = sum * mine + other.y * theirs;
+            m = m_new;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[n] = o[n] * mine + lo4[n * 64] * theirs;
+        }
+    }
+    if (tg != 0 || !live) return;
     // lane: row col, dimensions (4 quarter + i) * NT + n
     const int64_t at = row * p.q_heads + hq;
+    const float m2 = m == -INFINITY ? m : m * scale2;
     if (p.splits > 1) {
         const int64_t part = at * p.splits + split;
-        if (quarter == 0) {
-            p.part_ml[2 * part] = m;
-            p.part_ml[2 * part + 1] = sum;
-        }
+        if (quarter == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * part) = float2{m2, sum};
         if (sum == 0.f) return;
         float* po = p.part_o + part * D;
 #pragma unroll
@@ -364,7 +603,7 @@ __global__ __launch_bounds__(kWaves * 64) void few_rows_kernel(AttnParams p) {
         return;
     }
     const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;   // NaN stays
-    if (p.lse && quarter == 0) p.lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
+    if (p.lse && quarter == 0) p.lse[at] = sum == 0.f ? -INFINITY : (m2 + log2f(sum)) * kLn2;
     uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at * D);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -373,51 +612,76 @@ __global__ __launch_bounds__(kWaves * 64) void few_rows_kernel(AttnParams p) {
             out[((4 * quarter + i) * NT + n) / 2] = pack2<E>(o[n][i] * inv, o[n + 1][i] * inv);
 }
 
-// One wave per served query row and head: its splits joined in order.
+// One workgroup per served query row and head: its splits, eight or four at a
+// time, joined in a fixed order.
 template <class E, int D>
-__global__ __launch_bounds__(256) void combine_kernel(AttnParams p, int64_t rows) {
-    const int lane = threadIdx.x & 63;
-    const int64_t job = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (job >= rows) return;
-    const int hq = (int)(job % p.q_heads);
-    const int b = (int)(job / p.q_heads / p.max_q), i = (int)(job / p.q_heads % p.max_q);
+__global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
+    constexpr int kPer = D / 4;            // threads of a split: four dimensions each
+    constexpr int kAt = 256 / kPer;        // splits at a time
+    __shared__ float4 acc_l[256];
+    __shared__ float sum_l[kAt], top_l[4];
+    const int hq = (int)(blockIdx.x % (uint32_t)p.q_heads);
+    const int job = (int)(blockIdx.x / (uint32_t)p.q_heads), b = job / p.max_q, i = job % p.max_q;
     const Rows r = rows_of(p, b);
     if (i >= r.shown) return;
     const int64_t at = (r.q0 + i) * p.q_heads + hq;
-    const float* ml = p.part_ml + 2 * at * p.splits;
+    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + at * p.splits;
     float m = -INFINITY;
-    for (int s = lane; s < p.splits; s += 64) m = fmaxf(m, ml[2 * s + 1] == 0.f ? -INFINITY : ml[2 * s]);
+    for (int s = threadIdx.x; s < p.splits; s += 256) {
+        const float2 v = ml[s];
+        m = fmaxf(m, v.y == 0.f ? -INFINITY : v.x);
+    }
     for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    if ((threadIdx.x & 63) == 0) top_l[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(top_l[0], top_l[1]), fmaxf(top_l[2], top_l[3]));
     const float base = m == -INFINITY ? 0.f : m;
-    float acc[D / 64] = {}, sum = 0.f;
-    for (int s = 0; s < p.splits; ++s) {
-        const float part = ml[2 * s + 1];
-        if (part == 0.f) continue;
-        const float w = exp2f(ml[2 * s] - base);
-        sum += w * part;
-        const float* po = p.part_o + (at * p.splits + s) * D + lane * (D / 64);
+    const int lane = threadIdx.x % kPer, first = threadIdx.x / kPer;
+    const float4* po = reinterpret_cast<const float4*>(p.part_o + at * p.splits * D) + lane;
+    float4 acc = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+#pragma unroll 4
+    for (int s = first; s < p.splits; s += kAt) {
+        const float2 v = ml[s];
+        if (v.y == 0.f) continue;          // a split that saw nothing wrote no part
+        const float w = __builtin_amdgcn_exp2f(v.x - base);
+        const float4 x = po[(int64_t)s * kPer];
+        sum += w * v.y;
+        acc.x += w * x.x, acc.y += w * x.y, acc.z += w * x.z, acc.w += w * x.w;
+    }
+    acc_l[threadIdx.x] = acc;
+    if (lane == 0) sum_l[first] = sum;
+    __syncthreads();
+    if (first != 0) return;
+    sum = 0.f;
+    acc = float4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) acc[i] += w * po[i];
+    for (int s = 0; s < kAt; ++s) {
+        const float4 x = acc_l[s * kPer + lane];
+        acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
+        sum += sum_l[s];
     }
     const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
     if (p.lse && lane == 0) p.lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
-    E* out = static_cast<E*>(p.out) + at * D + lane * (D / 64);
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) out[i] = (E)(acc[i] * inv);
+    uint2* out = reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at * D) + lane;
+    *out = uint2{pack2<E>(acc.x * inv, acc.y * inv), pack2<E>(acc.z * inv, acc.w * inv)};
 }
 
 template <class E, int D>
 gvr_status launch(const AttnParams& p, void* stream) {
-    const dim3 grid((unsigned)((p.jobs + kWaves - 1) / kWaves)), block(kWaves * 64);
-    if (p.selection)
-        hipLaunchKernelGGL((few_rows_kernel<E, D, true>), grid, block, 0, (hipStream_t)stream, p);
+    const int waves = 1 << (p.hw_shift + p.tw_shift);
+    const dim3 grid((unsigned)p.jobs), block(waves * 64);
+    const bool gather = p.selection || p.page_shift < 4;
+    const size_t join = p.tw_shift ? (size_t)(waves / 2) * (D / 16 * 1024 + 512) : 0;
+    const size_t lds = gather && join < kSlots * 8 ? kSlots * 8 : join;
+    if (gather)
+        hipLaunchKernelGGL((few_rows_kernel<E, D, true>), grid, block, lds, (hipStream_t)stream, p);
     else
-        hipLaunchKernelGGL((few_rows_kernel<E, D, false>), grid, block, 0, (hipStream_t)stream, p);
+        hipLaunchKernelGGL((few_rows_kernel<E, D, false>), grid, block, lds, (hipStream_t)stream, p);
     if (hipGetLastError() != hipSuccess) return GVR_ERR_HIP;
     if (p.splits > 1) {
-        const int64_t rows = (int64_t)p.sequences * p.max_q * p.q_heads;
-        hipLaunchKernelGGL((combine_kernel<E, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, (hipStream_t)stream, p,
-                           rows);
+        hipLaunchKernelGGL((combine_kernel<E, D>), dim3((unsigned)((int64_t)p.sequences * p.max_q * p.q_heads)), dim3(256),
+                           0, (hipStream_t)stream, p);
         if (hipGetLastError() != hipSuccess) return GVR_ERR_HIP;
     }
     return GVR_OK;
@@ -455,19 +719,21 @@ gvr_status gvr_kv4_attention(const gvr_kv4_cache* cache, const gvr_kv4_attention
     if (!a.q || !a.out || !a.ctx_len || (!a.block_table && a.table_width > 0)) return GVR_ERR_INVALID_ARG;
     if (((uintptr_t)a.q | (uintptr_t)a.out) & 15) return GVR_ERR_INVALID_ARG;
     const gvr_kv4::AttnPlan plan = gvr_kv4::plan_attention(*cache, a, ws_bytes);
-    if (plan.jobs > gvr_kv4::kMaxCount || a.T * a.q_heads > gvr_kv4::kMaxCount) return GVR_ERR_TOO_LONG;
+    if (plan.jobs > gvr_kv4::kMaxCount || (int64_t)a.sequences * plan.max_q * a.q_heads > gvr_kv4::kMaxCount)
+        return GVR_ERR_TOO_LONG;
     AttnParams p;
     p.cache = cache->data;
     p.q = a.q, p.qt = a.q_token_stride, p.qh = a.q_head_stride;
     p.out = a.out, p.lse = a.lse;
     p.block_table = a.block_table, p.ctx_len = a.ctx_len, p.q_start = a.q_start, p.selection = a.selection;
-    p.table_width = a.table_width, p.pages = cache->pages, p.T = a.T;
+    p.table_width = a.table_width, p.pages = (int32_t)cache->pages, p.T = a.T;
     p.record = gvr_kv4::record_bytes(cache->kv_heads, cache->head_dim);
     p.page_shift = gvr_kv4::log2_of(cache->page_size);
     p.kv_heads = cache->kv_heads, p.q_heads = a.q_heads, p.group = a.q_heads / cache->kv_heads;
     p.sequences = a.sequences;
     p.uniform_q = a.q_start ? 0 : (int32_t)(a.T / a.sequences);
     p.max_q = plan.max_q, p.tiles = plan.tiles, p.jobs = plan.jobs, p.splits = plan.splits, p.chunk = plan.chunk;
+    p.hw_shift = plan.hw_shift, p.tw_shift = plan.tw_shift;
     p.K = a.K, p.causal = a.causal;
     p.scale2 = a.scale * kLog2e;
     p.part_o = static_cast<float*>(workspace);

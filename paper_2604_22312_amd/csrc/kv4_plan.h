@@ -49,22 +49,25 @@ inline gvr_status check_attention(const gvr_kv4_cache& c, const gvr_kv4_attentio
     return GVR_OK;
 }
 
-constexpr int kRows = 16;         // query rows of a wave
-constexpr int kStep = 32;         // tokens of a wave's step
-constexpr int kWaves = 4;         // waves of a workgroup
-constexpr int kMinChunk = 128;    // fewest tokens of a split
-constexpr int kFillWaves = 4096;  // waves that fill the device
+constexpr int kRows = 16;          // query rows of a wave
+constexpr int kStep = 32;          // tokens of a wave's step
+constexpr int kMaxWaves = 8;       // of a workgroup
+constexpr int kSlots = 2048;       // tokens whose places a workgroup holds in LDS
+constexpr int kFillWaves = 4096;   // waves that fill the device
+constexpr int kMinSteps = 4;       // fewest steps of a wave worth another split
 
 struct AttnPlan {
     int max_q;        // query tokens of a sequence
     int tiles;        // row tiles of a sequence and KV head
-    int64_t jobs;     // waves
+    int hw_shift;     // log2 of the KV heads of a workgroup
+    int tw_shift;     // log2 of the waves that share a head's steps
+    int64_t jobs;     // workgroups
     int splits;       // of a context or selection
     int chunk;        // tokens of a split
     size_t ws_bytes;
 };
 
-inline size_t partial_bytes(int64_t T, int q_heads, int head_dim, int splits) {
+inline size_t partial_bytes(int64_t T, int q_heads, int head_dim, int64_t splits) {
     return splits > 1 ? (size_t)T * q_heads * splits * (head_dim + 2) * 4 : 0;
 }
 
@@ -75,22 +78,35 @@ inline AttnPlan plan_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_a
     if (p.max_q > a.T) p.max_q = (int)a.T;
     const int64_t tiles = a.selection ? (int64_t)p.max_q * ((G + kRows - 1) / kRows)
                                       : ((int64_t)p.max_q * G + kRows - 1) / kRows;
-    p.tiles = (int)tiles;
+    p.tiles = (int)(tiles > kMaxCount ? kMaxCount : tiles);
     const int64_t n = a.selection ? a.K : a.table_width * c.page_size;
-    const int64_t units = (int64_t)a.sequences * tiles * c.kv_heads;
-    int64_t splits = units > 0 ? (kFillWaves + units - 1) / units : 1;
-    const int64_t most = (n + kMinChunk - 1) / kMinChunk;
-    splits = splits > most ? most : splits;
-    splits = splits < 1 ? 1 : splits > 1024 ? 1024 : splits;
-    while (splits > 1 && partial_bytes(a.T, a.q_heads, c.head_dim, (int)splits) > ws_bytes) --splits;
+    const int64_t steps = (n + kStep - 1) / kStep;
+    const int64_t units = (int64_t)a.sequences * tiles;
+    const int64_t heads = units * c.kv_heads;
+    // waves wanted for each head of a unit
+    int64_t want = heads > 0 ? (kFillWaves + heads - 1) / heads : 1;
+    const int64_t most = (steps + kMinSteps - 1) / kMinSteps;
+    want = want > most ? most : want;
+    if (want < 1) want = 1;
+    p.hw_shift = p.tw_shift = 0;
+    if (steps <= kMaxWaves * kMinSteps) {
+        // a short context: one workgroup joins its waves, and no second kernel runs
+        while ((1 << p.tw_shift) < kMaxWaves && (1 << p.tw_shift) < want) ++p.tw_shift;
+    }
+    while (p.hw_shift + p.tw_shift < log2_of(kMaxWaves) && c.kv_heads % (2 << p.hw_shift) == 0) ++p.hw_shift;
+    while (p.hw_shift + p.tw_shift < log2_of(kMaxWaves) && (1 << p.tw_shift) < want) ++p.tw_shift;
+    int64_t splits = (want + (1 << p.tw_shift) - 1) >> p.tw_shift;
+    if (splits > 1024) splits = 1024;
+    while (splits > 1 && partial_bytes(a.T, a.q_heads, c.head_dim, splits) > ws_bytes) --splits;
+    const int64_t unit = (int64_t)kStep << p.tw_shift;
     int64_t chunk = (n + splits - 1) / splits;
-    chunk = (chunk + kStep - 1) / kStep * kStep;
-    if (chunk < kStep) chunk = kStep;
+    chunk = (chunk + unit - 1) / unit * unit;
+    if (chunk < unit) chunk = unit;
     splits = n > 0 ? (n + chunk - 1) / chunk : 1;
-    p.chunk = (int)(chunk > kMaxCount ? kMaxCount / kStep * kStep : chunk);
+    p.chunk = (int)(chunk > kMaxCount ? kMaxCount / unit * unit : chunk);
     p.splits = (int)splits;
-    p.jobs = units * splits;
-    p.ws_bytes = partial_bytes(a.T, a.q_heads, c.head_dim, p.splits);
+    p.jobs = units * (c.kv_heads >> p.hw_shift) * splits;
+    p.ws_bytes = partial_bytes(a.T, a.q_heads, c.head_dim, splits);
     return p;
 }
 
