@@ -44,8 +44,9 @@ namespace {
 
 using gvr_kv4::kRows;
 using gvr_kv4::kStep;
-using gvr_kv4::kMaxWaves;
+using gvr_kv4::kThreads;
 using gvr_kv4::kSlots;
+using gvr_kv4::kMaxSplits;
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
@@ -255,32 +256,45 @@ DEV Rows rows_of(const AttnParams& p, int b) {
     return r;
 }
 
-// What a wave loads for a step of 32 tokens.
+// LDS of a wave: the codes of V of its 32 tokens (16-byte chunks, see v_place)
+// and the scale bytes of K and V; of a workgroup: its waves', then slots.
 template <int D>
-struct Step {
-    static constexpr int kRuns = D == 256 ? 2 : 1;
-    static constexpr int kVWords = D == 256 ? 2 : 1;
-    v4u k[2][kRuns];          // codes of the token of this lane's column
-    uint32_t ks[2][kRuns];    // their scale bytes
-    Codes<D / 32> v[8];       // codes of the lane's eight tokens
-    uint32_t vs[8];           // their scale bytes
-    uint32_t there;           // bit n: token n exists
-    int t0;
+struct WaveLds {
+    static constexpr int kCodes = kStep * D / 2;
+    static constexpr int kScales = kStep * D / 32;     // of K, then as many of V
+    static constexpr int kBytes = kCodes + 2 * kScales;
+    static constexpr int kLds = gvr_kv4::kWaves * kBytes + kSlots * 4;   // and the queries of the workgroup's heads
 };
 
-// GATHER: the tokens' slots come from LDS (a selection, or pages of fewer than
-// 16 tokens); else from two page numbers per step.
-template <class E, int D, bool GATHER>
-__global__ __launch_bounds__(kMaxWaves * 64, 2) void few_rows_kernel(AttnParams p) {
+// Byte of chunk `chunk` of V's codes of token tok (0 .. 31): tokens 4 q + i of
+// 16 lie in the order i, q, so that the quarters read side by side, and the
+// chunks of a token are turned by i, so that a write of 16 tokens meets all banks.
+template <int D>
+DEV int v_place(int tok, int chunk) {
+    const int i = tok & 3;
+    return ((tok & ~15) + 4 * i + ((tok >> 2) & 3)) * (D / 2) + (chunk ^ (D == 64 ? i & 1 : i)) * 16;
+}
+
+DEV void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <class E, int D>
+__global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(AttnParams p) {
     constexpr int NT = D / 16;        // dimensions of V per lane = matrix steps of the second product
     typedef Query<E, D> Q;
-    extern __shared__ uint8_t lds[];
+    typedef WaveLds<D> L;
+    extern __shared__ __align__(16) uint8_t lds[];
     const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tg = wave >> p.hw_shift;                    // turn of this wave at the steps
+    const int hl = wave & ((1 << p.hw_shift) - 1);        // head of the workgroup's
+    const int tg = wave >> p.hw_shift;                    // part of the tile's tokens
+    const int tt_shift = 5 + p.tw_shift, TT = 1 << tt_shift;   // tokens of a tile
     uint32_t job = blockIdx.x;
     const int groups = p.kv_heads >> p.hw_shift;
-    const int h = (int)(job % (uint32_t)groups << p.hw_shift) + (wave & ((1 << p.hw_shift) - 1));
+    const int h0 = (int)(job % (uint32_t)groups) << p.hw_shift, h = h0 + hl;
     job /= (uint32_t)groups;
     const int tile = (int)(job % (uint32_t)p.tiles);
     job /= (uint32_t)p.tiles;
@@ -293,21 +307,20 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void few_rows_kernel(AttnParams 
     if (shown <= 0) return;
     const int64_t held = p.table_width << p.page_shift;
     const int ctx = p.pages > 0 ? (int)min((int64_t)max(p.ctx_len[b], 0), held) : 0;
-    const bool sel = GATHER && p.selection;
 
     // this lane's query row; tokens [0, end) of the context or selection concern the tile
     int qi, qg, end, sel_last = 0;
     bool live;
     const int32_t* list = nullptr;
-    if (sel) {
-        const int per = (p.group + kRows - 1) / kRows;
-        qi = tile / per;
-        qg = (tile - qi * per) * kRows + col;
-        if (qi >= shown) return;
+    if (p.selection) {
+        const int per = (p.group + kRows - 1) / kRows, token = tile / per;
+        if (token >= shown) return;
+        qi = token;
+        qg = (tile - token * per) * kRows + col;
         live = qg < p.group;
         end = p.pages > 0 ? p.K : 0;
-        list = p.selection + (q0 + qi) * p.K;
-        sel_last = p.causal ? (int)(ctx - nq + qi) : ctx - 1;
+        list = p.selection + (q0 + token) * p.K;
+        sel_last = p.causal ? (int)(ctx - nq + token) : ctx - 1;
     } else {
         const int r = tile * kRows + col;
         qi = r / p.group;
@@ -320,23 +333,66 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void few_rows_kernel(AttnParams 
     const int64_t row = q0 + qi;
     const int hq = h * p.group + qg;
     // last token that this lane's row sees, and the last that all of the tile's rows see
-    const int last = !live ? -1 : sel ? 0x7FFFFFFF : p.causal ? (int)(ctx - nq + qi) : ctx - 1;
-    const int all_last = sel ? 0x7FFFFFFF
-                             : (int)max((int64_t)-1, p.causal ? ctx - nq + (tile * kRows) / p.group : (int64_t)ctx - 1);
+    const int last = !live ? -1 : list ? 0x7FFFFFFF : p.causal ? (int)(ctx - nq + qi) : ctx - 1;
+    const int all_last = list ? 0x7FFFFFFF
+                              : (int)max((int64_t)-1, p.causal ? ctx - nq + (tile * kRows) / p.group : (int64_t)ctx - 1);
     const int64_t lo = (int64_t)split * p.chunk;
     const int begin = (int)min(lo, (int64_t)end), stop = (int)min(lo + p.chunk, (int64_t)end);
 
     const float scale2 = fabsf(p.scale2);
-    const Q q = load_query<E, D>(live ? static_cast<const E*>(p.q) + row * p.qt + hq * p.qh : nullptr,
-                                 p.scale2 < 0.f ? -1.f : 1.f, lane);
+    const E* const q_row = live ? static_cast<const E*>(p.q) + row * p.qt + hq * p.qh : nullptr;
     const uint32_t record = (uint32_t)p.record;
-    const uint32_t k_off = h * (D / 2) + 16 * (D == 64 ? quarter & 1 : quarter);
-    const uint32_t v_off = (p.kv_heads + h) * (D / 2) + col * (D / 32);
-    const uint32_t ks_off = p.kv_heads * D + h * (D / 32) + (D == 64 ? quarter & 1 : quarter);
-    const uint32_t vs_off = p.kv_heads * D + (p.kv_heads + h) * (D / 32) + col * (D / 16) / 32;
     const int32_t* table = p.block_table + (int64_t)b * p.table_width;
     const int page_mask = (1 << p.page_shift) - 1;
-    const int stride = kStep << p.tw_shift;
+
+    // The lane loads 16-byte chunk `quarter` of K and V of token `col` of each
+    // half of a step (D = 64: the quarters 2, 3 repeat 0, 1; D = 256: chunk
+    // quarter + 4 too), and from the scales those of K or V.
+    constexpr int kRuns = D == 256 ? 2 : 1;
+    const int chunk = D == 64 ? quarter & 1 : quarter;
+    const uint8_t* const k_src = p.cache + (uint32_t)(h * (D / 2) + chunk * 16);
+    const uint8_t* const v_src = p.cache + (uint32_t)((p.kv_heads + h) * (D / 2) + chunk * 16);
+    const uint8_t* const s_src = p.cache + (uint32_t)(p.kv_heads * D + ((quarter & 1 ? p.kv_heads : 0) + h) * (D / 32));
+    uint8_t* const mine = lds + wave * L::kBytes;
+    int32_t* const slots = reinterpret_cast<int32_t*>(lds + gvr_kv4::kWaves * L::kBytes);
+    // The head's queries stay in LDS (16 bytes a lane side by side): they are
+    // needed once a step, and their registers are worth a second workgroup.
+    v4u* const q_lds = reinterpret_cast<v4u*>(lds + L::kLds) + hl * (Q::kRuns * Q::kPer * 2 * 64) + lane;
+    uint32_t q_scale[Q::kRuns * Q::kPer];
+    auto query = [&](int i) {
+        const v4u a = q_lds[i * 128], b = q_lds[i * 128 + 64];
+        return v8i{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+    };
+    struct Step {
+        v4u k[2][kRuns], v[2][kRuns];
+        Codes<D / 32> s[2];
+        uint32_t there;   // bit n: token n exists
+    };
+    auto fetch = [&](int t_lds, Step& d) {   // the step at slot t_lds of the piece
+        d.there = 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int slot = slots[t_lds + 16 * t + col];
+            d.there |= ((uint32_t)__ballot(slot >= 0) & 0xFFFFu) << (16 * t);
+            const uint64_t at = (uint64_t)(uint32_t)max(slot, 0) * record;
+#pragma unroll
+            for (int c = 0; c < kRuns; ++c) {
+                d.k[t][c] = load16(k_src + at + 64 * c);
+                d.v[t][c] = load16(v_src + at + 64 * c);
+            }
+            d.s[t] = load_codes<D / 32>(s_src + at);
+        }
+    };
+    // Where the lane writes and reads in its wave's LDS (t: constants).
+    const int vw_at = v_place<D>(col, chunk), sw_at = L::kCodes + (quarter & 1) * L::kScales + col * (D / 32);
+    const int ks_at = L::kCodes + col * (D / 32) + chunk;
+    const int vs_at = L::kCodes + L::kScales + 4 * quarter * (D / 32) + col * (D / 16) / 32;
+    int vr_at[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int byte = col * (D / 32);
+        vr_at[i] = v_place<D>(4 * quarter + i, byte / 16) + byte % 16;
+    }
 
     float m = -INFINITY, limit = -INFINITY, base = 0.f, sum = 0.f;
     // maximum (of unscaled scores) that the weights refer to, the score that moves it, maximum * scale2
@@ -344,93 +400,51 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void few_rows_kernel(AttnParams 
 #pragma unroll
     for (int n = 0; n < NT; ++n) o[n] = v4f{0.f, 0.f, 0.f, 0.f};
 
-    // Slots of a step's two runs of 16 tokens from page numbers (scalar). A
-    // run that is not there, and a run's tokens past its end, read records
-    // that are in the cache (a page of 16 or more holds the whole run).
-    // The loads go through a buffer resource over the run: a lane's offset is
-    // a constant, and what a scalar adds costs no vector instruction.
-    const int ko = (int)(col * record + k_off), kso = (int)(col * record + ks_off);
-    const int vo = (int)(4 * quarter * record + v_off), vso = (int)(4 * quarter * record + vs_off);
-    auto fetch_dense = [&](int t0, Step<D>& d) {
-        d.t0 = t0;
-        d.there = 0;
-        __amdgpu_buffer_rsrc_t run[2];
+    // t0: first token (or place in the list) of the step; its registers take
+    // the step at slot t_next when they are free.
+    auto use = [&](Step& d, int t0, int t_next) {
+        const uint32_t there = d.there;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int tok = t0 + 16 * t;
-            const int n = min(stop - tok, 16);   // tokens of this run
-            const int page = n > 0 ? table[tok >> p.page_shift] : -1;
-            const bool ok = (uint32_t)page < (uint32_t)p.pages;
-            if (ok) d.there |= (n >= 16 ? 0xFFFFu : (1u << n) - 1u) << (16 * t);
-            const uint64_t slot = ok ? (uint32_t)((page << p.page_shift) + (tok & page_mask)) : 0u;
-            run[t] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p.cache) + slot * record, (short)0,
-                                                       (int)(16 * record), kBufWord3);
+#pragma unroll
+            for (int c = 0; c < kRuns; ++c)
+                *reinterpret_cast<v4u*>(mine + (vw_at ^ (64 * c)) + 16 * t * (D / 2)) = d.v[t][c];
+            uint8_t* sw = mine + sw_at + 16 * t * (D / 32);
+            if constexpr (D == 64)
+                *reinterpret_cast<uint16_t*>(sw) = (uint16_t)d.s[t].w[0];
+            else if constexpr (D == 128)
+                *reinterpret_cast<uint32_t*>(sw) = d.s[t].w[0];
+            else
+                *reinterpret_cast<v2u*>(sw) = v2u{d.s[t].w[0], d.s[t].w[1]};
         }
+        v4f sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int i = Q::kRuns * Q::kPer - 1; i >= 0; --i) {   // (D = 64: runs of the same K; else terms, then runs of K)
+            const int c = D == 64 ? 0 : i / Q::kPer;
+            const v8i qi8 = query(i);
 #pragma unroll
-            for (int c = 0; c < Step<D>::kRuns; ++c) {
-                d.k[t][c] = __builtin_amdgcn_raw_buffer_load_b128(run[t], ko + 64 * c, 0, 0);
-                d.ks[t][c] = __builtin_amdgcn_raw_buffer_load_b8(run[t], kso + 4 * c, 0, 0);
-            }
+            for (int t = 0; t < 2; ++t)
+                sc[t] = mfma_mx(d.k[t][c], mine[ks_at + 16 * t * (D / 32) + 4 * c], qi8, q_scale[i], sc[t]);
+        }
+        fetch(t_next, d);
+        Codes<D / 32> v[8];
+        float vs[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int at = (j & 3) * (int)record;
-            if constexpr (D == 64) {
-                d.v[j].w[0] = __builtin_amdgcn_raw_buffer_load_b16(run[j >> 2], vo, at, 0);
-            } else if constexpr (D == 128) {
-                d.v[j].w[0] = __builtin_amdgcn_raw_buffer_load_b32(run[j >> 2], vo, at, 0);
-            } else {
-                const v2u v = __builtin_amdgcn_raw_buffer_load_b64(run[j >> 2], vo, at, 0);
-                d.v[j].w[0] = v[0], d.v[j].w[1] = v[1];
+            const uint8_t* vp = mine + vr_at[j & 3] + 16 * (j >> 2) * (D / 2);
+            if constexpr (D == 64)
+                v[j].w[0] = *reinterpret_cast<const uint16_t*>(vp);
+            else if constexpr (D == 128)
+                v[j].w[0] = *reinterpret_cast<const uint32_t*>(vp);
+            else {
+                const v2u w = *reinterpret_cast<const v2u*>(vp);
+                v[j].w[0] = w[0], v[j].w[1] = w[1];
             }
-            d.vs[j] = __builtin_amdgcn_raw_buffer_load_b8(run[j >> 2], vso, at, 0);
+            vs[j] = scale_of(mine[vs_at + (16 * (j >> 2) + (j & 3)) * (D / 32)]);
         }
-    };
-    // From record offsets in LDS (-1: not there).
-    const int64_t* offs = reinterpret_cast<const int64_t*>(lds);
-    const uint8_t *const kp = p.cache + k_off, *const ksp = p.cache + ks_off, *const vp = p.cache + v_off,
-                         *const vsp = p.cache + vs_off;
-    auto fetch_gather = [&](int t0, int t_lds, bool in, Step<D>& d) {
-        d.t0 = t0;
-        t_lds = in ? t_lds : 0;
-        d.there = in ? (uint32_t)__ballot(offs[t_lds + (lane & 31)] >= 0) : 0u;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int64_t at = max(offs[t_lds + 16 * t + col], (int64_t)0);
-#pragma unroll
-            for (int c = 0; c < Step<D>::kRuns; ++c) {
-                d.k[t][c] = load16(kp + at + 64 * c);
-                d.ks[t][c] = ksp[at + 4 * c];
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int64_t at = max(offs[t_lds + 16 * (j >> 2) + 4 * quarter + (j & 3)], (int64_t)0);
-            d.v[j] = load_codes<D / 32>(vp + at);
-            d.vs[j] = vsp[at];
-        }
-    };
-
-    auto use = [&](Step<D>& d) {
-        if (d.there == 0) return;
-        v4f sc[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            v4f acc = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (D == 64) {
-#pragma unroll
-                for (int r = 0; r < Q::kRuns; ++r) acc = mfma_mx(d.k[t][0], d.ks[t][0], q.b[r][0], q.scale[r][0], acc);
-            } else {
-#pragma unroll
-                for (int c = 0; c < Q::kRuns; ++c)
-#pragma unroll
-                    for (int u = Q::kPer - 1; u >= 0; --u)
-                        acc = mfma_mx(d.k[t][c], d.ks[t][c], q.b[c][u], q.scale[c][u], acc);
-            }
-            sc[t] = acc;
-        }
-        const bool full = d.there == 0xFFFFFFFFu && d.t0 + kStep - 1 <= all_last;   // wave-uniform
+        const bool full = there == 0xFFFFFFFFu && t0 + kStep - 1 <= all_last;   // wave-uniform
+        int quarter_now = quarter;   // (its multiples are not worth registers through the loop)
+        asm("" : "+v"(quarter_now));
         uint32_t seen = 0xFFu;   // bit 4 t + i: this row sees token 16 t + 4 quarter + i
         if (!full) {
             seen = 0;
@@ -438,8 +452,8 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void few_rows_kernel(AttnParams 
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int n = 16 * t + 4 * quarter + i;
-                    const bool see = ((d.there >> n) & 1) && d.t0 + n <= last;
+                    const int n = 16 * t + 4 * quarter_now + i;
+                    const bool see = ((there >> n) & 1) && t0 + n <= last;
                     seen |= see ? 1u << (4 * t + i) : 0u;
                     if (!see) sc[t][i] = -INFINITY;
                 }
@@ -462,9 +476,6 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void few_rows_kernel(AttnParams 
         float w[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j >> 2][j & 3], scale2, -base));
-        float vs[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) vs[j] = scale_of(d.vs[j]);
         if (!full) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) w[j] = (seen >> j) & 1 ? w[j] : 0.f;
@@ -475,12 +486,12 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void few_rows_kernel(AttnParams 
             uint32_t bad = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const bool here = (d.there >> (16 * (j >> 2) + 4 * quarter + (j & 3))) & 1;
+                const bool here = (there >> (16 * (j >> 2) + 4 * quarter_now + (j & 3))) & 1;
                 const bool nan = __float_as_uint(vs[j]) == 0x7F800000u;
                 bad |= here && nan ? 1u << j : 0u;
                 if (!here || nan) {
                     vs[j] = 0.f;
-                    d.v[j] = Codes<D / 32>{};
+                    v[j] = Codes<D / 32>{};
                 }
             }
             if (__any(bad != 0)) {
@@ -505,7 +516,7 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void few_rows_kernel(AttnParams 
         for (int n = 0; n < NT; n += 2) {
             uint32_t u[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = unpack<E>(d.v[j].w[n / 8], vs[j], (n % 8) / 2);
+            for (int j = 0; j < 8; ++j) u[j] = unpack<E>(v[j].w[n / 8], vs[j], (n % 8) / 2);
             v4u a0, a1;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -517,46 +528,44 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void few_rows_kernel(AttnParams 
         }
     };
 
-    // The loads of the next step go out before a step is used.
-    if constexpr (!GATHER) {
-        int t0 = begin + kStep * tg;
-        if (t0 < stop) {
-            Step<D> d[2];
-            fetch_dense(t0, d[0]);
-            for (; t0 < stop; t0 += 2 * stride) {
-                fetch_dense(t0 + stride, d[1]);
-                use(d[0]);
-                fetch_dense(t0 + 2 * stride, d[0]);
-                use(d[1]);
+    // Pieces of the chunk: slots into LDS, then step after step, the loads two
+    // steps ahead. The waves of a workgroup read different parts of the same
+    // records, so they are kept together: a line that one of them brought into
+    // the caches is used by the others before it leaves.
+    for (int piece = begin; piece < stop; piece += kSlots) {
+        const int fill = min(stop - piece, kSlots), padded = (fill + TT - 1) & -TT;
+        lds_barrier();   // the waves are through with the last piece
+        for (int i = threadIdx.x; i < padded; i += kThreads) {
+            int slot = -1;
+            if (i < fill) {
+                const int tok = list ? list[piece + i] : piece + i;
+                if (tok >= 0 && (!list || tok <= sel_last)) {
+                    const int page = table[tok >> p.page_shift];
+                    if ((uint32_t)page < (uint32_t)p.pages) slot = (page << p.page_shift) + (tok & page_mask);
+                }
             }
+            slots[i] = slot;
         }
-    } else {
-        for (int piece = begin; piece < stop; piece += kSlots) {
-            const int fill = min(stop - piece, kSlots);
-            __syncthreads();   // the waves are through with the last piece
-            for (int i = threadIdx.x; i < (fill + kStep - 1) / kStep * kStep; i += blockDim.x) {
-                int64_t at = -1;
-                if (i < fill) {
-                    const int tok = sel ? list[piece + i] : piece + i;
-                    if (tok >= 0 && (!sel || tok <= sel_last)) {
-                        const int page = table[tok >> p.page_shift];
-                        if ((uint32_t)page < (uint32_t)p.pages) at = (((int64_t)page << p.page_shift) + (tok & page_mask)) * record;
-                    }
-                }
-                reinterpret_cast<int64_t*>(lds)[i] = at;
-            }
-            __syncthreads();
-            int t = kStep * tg;
-            if (t < fill) {
-                Step<D> d[2];
-                fetch_gather(piece + t, t, true, d[0]);
-                for (; t < fill; t += 2 * stride) {
-                    fetch_gather(piece + t + stride, t + stride, t + stride < fill, d[1]);
-                    use(d[0]);
-                    fetch_gather(piece + t + 2 * stride, t + 2 * stride, t + 2 * stride < fill, d[0]);
-                    use(d[1]);
+        lds_barrier();
+        const int first = kStep * tg, final = padded - TT + first;
+        Step d;
+        fetch(first, d);
+        if (piece == begin) {   // while the first loads run
+            const Q q = load_query<E, D>(q_row, p.scale2 < 0.f ? -1.f : 1.f, lane);
+#pragma unroll
+            for (int i = 0; i < Q::kRuns * Q::kPer; ++i) {
+                const v8i b = q.b[i / Q::kPer][i % Q::kPer];
+                q_scale[i] = q.scale[i / Q::kPer][i % Q::kPer];
+                if (tg == 0) {
+                    q_lds[i * 128] = v4u{(uint32_t)b[0], (uint32_t)b[1], (uint32_t)b[2], (uint32_t)b[3]};
+                    q_lds[i * 128 + 64] = v4u{(uint32_t)b[4], (uint32_t)b[5], (uint32_t)b[6], (uint32_t)b[7]};
                 }
             }
+            lds_barrier();
+        }
+        for (int t = first; t < padded; t += TT) {
+            use(d, piece + t, min(t + TT, final));
+            __builtin_amdgcn_s_barrier();
         }
     }
     sum += __shfl_xor(sum, 16, 64);
@@ -612,14 +621,15 @@ __global__ __launch_bounds__(kMaxWaves * 64, 2) void few_rows_kernel(AttnParams 
             out[((4 * quarter + i) * NT + n) / 2] = pack2<E>(o[n][i] * inv, o[n + 1][i] * inv);
 }
 
-// One workgroup per served query row and head: its splits, eight or four at a
-// time, joined in a fixed order.
+// One workgroup per served query row and head: its splits joined in a fixed
+// order, `kAt` at a time. The weights are made first, so that the loads of the
+// parts wait for nothing.
 template <class E, int D>
 __global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
     constexpr int kPer = D / 4;            // threads of a split: four dimensions each
     constexpr int kAt = 256 / kPer;        // splits at a time
     __shared__ float4 acc_l[256];
-    __shared__ float sum_l[kAt], top_l[4];
+    __shared__ float weight_l[kMaxSplits], red_l[8];
     const int hq = (int)(blockIdx.x % (uint32_t)p.q_heads);
     const int job = (int)(blockIdx.x / (uint32_t)p.q_heads), b = job / p.max_q, i = job % p.max_q;
     const Rows r = rows_of(p, b);
@@ -632,34 +642,40 @@ __global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
         m = fmaxf(m, v.y == 0.f ? -INFINITY : v.x);
     }
     for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    if ((threadIdx.x & 63) == 0) top_l[threadIdx.x >> 6] = m;
+    if ((threadIdx.x & 63) == 0) red_l[threadIdx.x >> 6] = m;
     __syncthreads();
-    m = fmaxf(fmaxf(top_l[0], top_l[1]), fmaxf(top_l[2], top_l[3]));
+    m = fmaxf(fmaxf(red_l[0], red_l[1]), fmaxf(red_l[2], red_l[3]));
     const float base = m == -INFINITY ? 0.f : m;
+    float sum = 0.f;
+    for (int s = threadIdx.x; s < p.splits; s += 256) {
+        const float2 v = ml[s];
+        const float w = v.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(v.x - base);   // 0: it saw nothing and wrote no part
+        weight_l[s] = w;
+        sum += w * v.y;
+    }
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
+    if ((threadIdx.x & 63) == 0) red_l[4 + (threadIdx.x >> 6)] = sum;
+    __syncthreads();
+    sum = (red_l[4] + red_l[5]) + (red_l[6] + red_l[7]);
     const int lane = threadIdx.x % kPer, first = threadIdx.x / kPer;
     const float4* po = reinterpret_cast<const float4*>(p.part_o + at * p.splits * D) + lane;
     float4 acc = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-#pragma unroll 4
+#pragma unroll 8
     for (int s = first; s < p.splits; s += kAt) {
-        const float2 v = ml[s];
-        if (v.y == 0.f) continue;          // a split that saw nothing wrote no part
-        const float w = __builtin_amdgcn_exp2f(v.x - base);
+        const float w = weight_l[s];
         const float4 x = po[(int64_t)s * kPer];
-        sum += w * v.y;
-        acc.x += w * x.x, acc.y += w * x.y, acc.z += w * x.z, acc.w += w * x.w;
+        const bool seen = w != 0.f;        // (what was not written may be anything)
+        acc.x += seen ? w * x.x : 0.f, acc.y += seen ? w * x.y : 0.f;
+        acc.z += seen ? w * x.z : 0.f, acc.w += seen ? w * x.w : 0.f;
     }
     acc_l[threadIdx.x] = acc;
-    if (lane == 0) sum_l[first] = sum;
     __syncthreads();
     if (first != 0) return;
-    sum = 0.f;
     acc = float4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < kAt; ++s) {
         const float4 x = acc_l[s * kPer + lane];
         acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
-        sum += sum_l[s];
     }
     const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
     if (p.lse && lane == 0) p.lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
@@ -669,15 +685,10 @@ __global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
 
 template <class E, int D>
 gvr_status launch(const AttnParams& p, void* stream) {
-    const int waves = 1 << (p.hw_shift + p.tw_shift);
-    const dim3 grid((unsigned)p.jobs), block(waves * 64);
-    const bool gather = p.selection || p.page_shift < 4;
-    const size_t join = p.tw_shift ? (size_t)(waves / 2) * (D / 16 * 1024 + 512) : 0;
-    const size_t lds = gather && join < kSlots * 8 ? kSlots * 8 : join;
-    if (gather)
-        hipLaunchKernelGGL((few_rows_kernel<E, D, true>), grid, block, lds, (hipStream_t)stream, p);
-    else
-        hipLaunchKernelGGL((few_rows_kernel<E, D, false>), grid, block, lds, (hipStream_t)stream, p);
+    const int join = p.tw_shift ? gvr_kv4::kWaves / 2 * (D / 16 * 1024 + 512) : 0;   // bytes of the waves' join
+    const int queries = (Query<E, D>::kRuns * Query<E, D>::kPer * 2048) << p.hw_shift;
+    hipLaunchKernelGGL((few_rows_kernel<E, D>), dim3((unsigned)p.jobs), dim3(kThreads), max(join, WaveLds<D>::kLds + queries),
+                       (hipStream_t)stream, p);
     if (hipGetLastError() != hipSuccess) return GVR_ERR_HIP;
     if (p.splits > 1) {
         hipLaunchKernelGGL((combine_kernel<E, D>), dim3((unsigned)((int64_t)p.sequences * p.max_q * p.q_heads)), dim3(256),

@@ -51,10 +51,13 @@ inline gvr_status check_attention(const gvr_kv4_cache& c, const gvr_kv4_attentio
 
 constexpr int kRows = 16;          // query rows of a wave
 constexpr int kStep = 32;          // tokens of a wave's step
-constexpr int kMaxWaves = 8;       // of a workgroup
-constexpr int kSlots = 2048;       // tokens whose places a workgroup holds in LDS
-constexpr int kFillWaves = 4096;   // waves that fill the device
-constexpr int kMinSteps = 4;       // fewest steps of a wave worth another split
+constexpr int kWaves = 8;          // of a workgroup
+constexpr int kThreads = 64 * kWaves;
+constexpr int kSlots = 4096;       // tokens whose slots a workgroup holds in LDS
+constexpr int kMaxSplits = 1024;
+constexpr int kCus = 256;          // compute units, each with one workgroup at a time (D = 64: two)
+constexpr int kMinTiles = 4;       // fewest tiles of a workgroup worth another split
+constexpr int kShort = 64;         // steps of a context that one workgroup takes, so that no second kernel runs
 
 struct AttnPlan {
     int max_q;        // query tokens of a sequence
@@ -82,21 +85,26 @@ inline AttnPlan plan_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_a
     const int64_t n = a.selection ? a.K : a.table_width * c.page_size;
     const int64_t steps = (n + kStep - 1) / kStep;
     const int64_t units = (int64_t)a.sequences * tiles;
-    const int64_t heads = units * c.kv_heads;
-    // waves wanted for each head of a unit
-    int64_t want = heads > 0 ? (kFillWaves + heads - 1) / heads : 1;
-    const int64_t most = (steps + kMinSteps - 1) / kMinSteps;
-    want = want > most ? most : want;
-    if (want < 1) want = 1;
-    p.hw_shift = p.tw_shift = 0;
-    if (steps <= kMaxWaves * kMinSteps) {
-        // a short context: one workgroup joins its waves, and no second kernel runs
-        while ((1 << p.tw_shift) < kMaxWaves && (1 << p.tw_shift) < want) ++p.tw_shift;
+    // KV heads of a workgroup: all that divide evenly (a record's parts are then
+    // read together), fewer, with more waves to each, while that spares splits
+    // and the contexts still last for several tiles.
+    const int all = log2_of(kWaves);
+    p.hw_shift = 0;
+    while (p.hw_shift < all && c.kv_heads % (2 << p.hw_shift) == 0) ++p.hw_shift;
+    auto jobs = [&](int hw) { return units * (c.kv_heads >> hw); };
+    auto tiles_of = [&](int hw) { return (steps + (kWaves >> hw) - 1) / (kWaves >> hw); };
+    while (p.hw_shift > 0 && jobs(p.hw_shift) < kCus && tiles_of(p.hw_shift - 1) >= kMinTiles &&
+           (jobs(p.hw_shift - 1) >= kCus / 2 || steps <= kShort))
+        --p.hw_shift;
+    p.tw_shift = all - p.hw_shift;
+    const int64_t fill = c.head_dim == 64 ? 2 * kCus : kCus;
+    int64_t splits = 1;
+    if (jobs(p.hw_shift) < kCus && steps > kShort) {
+        splits = jobs(p.hw_shift) > 0 ? (fill + jobs(p.hw_shift) - 1) / jobs(p.hw_shift) : 1;
+        const int64_t most = (tiles_of(p.hw_shift) + kMinTiles - 1) / kMinTiles;
+        splits = splits > most ? most : splits;
     }
-    while (p.hw_shift + p.tw_shift < log2_of(kMaxWaves) && c.kv_heads % (2 << p.hw_shift) == 0) ++p.hw_shift;
-    while (p.hw_shift + p.tw_shift < log2_of(kMaxWaves) && (1 << p.tw_shift) < want) ++p.tw_shift;
-    int64_t splits = (want + (1 << p.tw_shift) - 1) >> p.tw_shift;
-    if (splits > 1024) splits = 1024;
+    if (splits > kMaxSplits) splits = kMaxSplits;
     while (splits > 1 && partial_bytes(a.T, a.q_heads, c.head_dim, splits) > ws_bytes) --splits;
     const int64_t unit = (int64_t)kStep << p.tw_shift;
     int64_t chunk = (n + splits - 1) / splits;
