@@ -73,6 +73,7 @@ struct AttnParams {
     int64_t table_width, record, T, jobs;
     int32_t page_shift, kv_heads, q_heads, group, sequences, uniform_q, max_q, tiles, splits, chunk, K, causal;
     int32_t pages;
+    int32_t many;
     int32_t hw_shift, tw_shift;   // log2 of a workgroup's KV heads, and of the waves that share a head's steps
     float scale2;     // scale * log2(e)
 };
@@ -114,13 +115,10 @@ DEV uint32_t pack2(float a, float b) {
     v[0] = (E)a, v[1] = (E)b;
     return __builtin_bit_cast(uint32_t, v);
 }
-// The largest of three (without the compiler's quieting of each operand: what
-// a NaN gives does not matter, its weight is NaN in any case).
-DEV float max3(float a, float b, float c) {
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
+// The largest; NaN if one of them is (then the row's weights are NaN in any
+// case). Unlike fmaxf this needs no quieting of each operand first.
+DEV float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+DEV float max3(float a, float b, float c) { return max2(max2(a, b), c); }
 DEV float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // NB bytes of codes as dwords (records are 4-byte aligned, runs of 2 bytes 2-byte).
@@ -400,6 +398,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
 #pragma unroll
     for (int n = 0; n < NT; ++n) o[n] = v4f{0.f, 0.f, 0.f, 0.f};
 
+    uint32_t nan_blocks = 0;   // the row sees a value that is NaN in this lane's dimensions (D = 256: lower, upper half)
     // t0: first token (or place in the list) of the step; its registers take
     // the step at slot t_next when they are free.
     auto use = [&](Step& d, int t0, int t_next) {
@@ -458,8 +457,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
                     if (!see) sc[t][i] = -INFINITY;
                 }
         }
-        float top = max3(max3(max3(sc[0][0], sc[0][1], sc[0][2]), sc[0][3], sc[1][0]), sc[1][1],
-                         fmaxf(sc[1][2], sc[1][3]));
+        float top = max2(max3(max3(sc[0][0], sc[0][1], sc[0][2]), sc[0][3], sc[1][0]),
+                         max3(sc[1][1], sc[1][2], sc[1][3]));
         if (__any(top > limit)) {
             top = fmaxf(top, __shfl_xor(top, 16, 64));
             top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -480,33 +479,27 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
 #pragma unroll
             for (int j = 0; j < 8; ++j) w[j] = (seen >> j) & 1 ? w[j] : 0.f;
             // A masked token's weight is zero, but a NaN block times zero is
-            // not. Tokens that are not there are taken as zeros. Where the
-            // rows see different tokens, a NaN block is taken out, and the
-            // rows that see it are found by a product of indicators.
-            uint32_t bad = 0;
+            // not: blocks that are NaN, and tokens that are not there, are
+            // taken as zeros, and the rows that see a NaN remember it.
+            bool bad = false;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const bool here = (there >> (16 * (j >> 2) + 4 * quarter_now + (j & 3))) & 1;
                 const bool nan = __float_as_uint(vs[j]) == 0x7F800000u;
-                bad |= here && nan ? 1u << j : 0u;
+                bad |= here && nan;
                 if (!here || nan) {
                     vs[j] = 0.f;
                     v[j] = Codes<D / 32>{};
                 }
             }
-            if (__any(bad != 0)) {
-                v4u ind, see;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    ind[j] = pack2<E>((bad >> (2 * j)) & 1 ? 1.f : 0.f, (bad >> (2 * j + 1)) & 1 ? 1.f : 0.f);
-                    see[j] = pack2<E>((seen >> (2 * j)) & 1 ? 1.f : 0.f, (seen >> (2 * j + 1)) & 1 ? 1.f : 0.f);
-                }
-                const v4f hits = mfma<E>(ind, see, v4f{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float nan = hits[i] > 0.f ? __builtin_nanf("") : 0.f;
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) o[n][i] += nan;
+            if (__any(bad)) {
+                // this lane's sums are of dimensions D / 4 quarter .. + D / 4
+                const uint8_t* vsb = mine + L::kCodes + L::kScales + D / 4 * quarter / 32;
+#pragma unroll 1
+                for (int n = 0; n < kStep; ++n) {
+                    uint32_t nan = vsb[n * (D / 32)] == 255 ? 1u : 0u;
+                    if constexpr (D == 256) nan |= vsb[n * (D / 32) + 1] == 255 ? 2u : 0u;
+                    nan_blocks |= ((there >> n) & 1) != 0 && t0 + n <= last ? nan : 0u;
                 }
             }
         }
@@ -570,6 +563,12 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
     }
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
+    if (nan_blocks) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[n][i] += (nan_blocks >> (D == 256 ? i / 2 : 0)) & 1 ? __builtin_nanf("") : 0.f;
+    }
 
     // Join the waves of a head: half of them hand theirs to the other half.
     for (int half = (1 << p.tw_shift) >> 1; half > 0; half >>= 1) {
@@ -619,6 +618,396 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
 #pragma unroll
         for (int n = 0; n < NT; n += 2)
             out[((4 * quarter + i) * NT + n) / 2] = pack2<E>(o[n][i] * inv, o[n + 1][i] * inv);
+}
+
+// ---- many query rows
+//
+// A workgroup of NW waves serves 32 NW query rows of one KV head, 32 per wave,
+// with the 32x32 matrix instructions; the products are those of the few-rows
+// kernel (a lane's column l % 32 is its row, half l / 32). The context goes
+// through LDS in tiles of 16 NW tokens: K as stored, V as 16-bit floats,
+// transposed (a row of tokens per dimension, in the order in which the
+// scores' registers name them), unpacked once for all the rows.
+template <int D, int NW>
+struct Many {
+    static constexpr int kThreads = 64 * NW;
+    static constexpr int kTile = 16 * NW;                  // tokens
+    static constexpr int kK = kTile * D / 2;               // bytes: codes of K
+    static constexpr int kV = kTile * D * 2;               // V
+    static constexpr int kS = kTile * D / 32;              // scale bytes of K, then of V
+    static constexpr int kBytes = kK + kV + 2 * kS;
+    static constexpr int kLds = 2 * kBytes + kSlots * 4 + 16;
+    static constexpr int kKLoads = kTile * D / 32;         // 16-byte chunks of K
+    static constexpr int kVLoads = kTile / 4 * (D / 8);    // 4 tokens x 8 dimensions of V
+    static constexpr int kSLoads = 2 * kTile;              // scale runs of K and of V
+    static constexpr int kKPer = (kKLoads + kThreads - 1) / kThreads;
+    static constexpr int kVPer = (kVLoads + kThreads - 1) / kThreads;
+};
+// Byte of a 16-byte chunk of K's codes, and of one of V's row of tokens: turned
+// so that 16 lanes beside each other meet all banks.
+template <int D>
+DEV int mk_place(int tok, int chunk) {
+    constexpr int kChunks = D / 32, kRows256 = 16 / kChunks;
+    return tok * (D / 2) + (chunk ^ ((tok / kRows256) & (kChunks - 1))) * 16;
+}
+template <int TILE>
+DEV int mv_place(int dim, int chunk) {
+    const int turn = TILE == 128 ? (dim ^ (dim >> 4)) & 15 : ((dim >> 1) ^ (dim >> 4)) & 7;
+    return dim * (2 * TILE) + (chunk ^ turn) * 16;
+}
+typedef float v16f __attribute__((ext_vector_type(16)));
+DEV v16f mfma_mx32(v4u a, uint32_t sa, v8i b, uint32_t sb, v16f c) {
+    const v8i a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b, c, kFp4, kFp8, 0, (int)sa, 0, (int)sb);
+}
+template <class E>
+DEV v16f mfma32(v4u a, v4u b, v16f c) {
+    typedef typename Vec<E>::x8 x8;
+    if constexpr (__is_same(E, __bf16))
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+}
+
+template <class E, int D, int NW>
+__global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(AttnParams p) {
+    typedef Many<D, NW> M;
+    constexpr int kTerms = __is_same(E, __bf16) ? 2 : 3;
+    constexpr int kRuns = D / 64, kDt = D / 32, kRowsWg = 32 * NW;
+    typedef typename Vec<E>::x8 x8;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // Workgroups of one KV head are a multiple of kv_heads apart: with 8 heads
+    // each XCD's cache holds one head's context. The last rows, which see the
+    // longest context, come first.
+    uint32_t job = blockIdx.x;
+    const int h = (int)(job % (uint32_t)p.kv_heads);
+    job /= (uint32_t)p.kv_heads;
+    const int split = (int)(job % (uint32_t)p.splits);
+    job /= (uint32_t)p.splits;
+    const int b = (int)(job % (uint32_t)p.sequences);
+    const int tile = p.tiles - 1 - (int)(job / (uint32_t)p.sequences);
+
+    const Rows rows = rows_of(p, b);
+    const int64_t q0 = rows.q0, nq = rows.nq;
+    const int shown = rows.shown;
+    const int first_row = tile * kRowsWg;
+    if (shown <= 0 || first_row / p.group >= shown) return;
+    const int64_t held = p.table_width << p.page_shift;
+    const int ctx = p.pages > 0 ? (int)min((int64_t)max(p.ctx_len[b], 0), held) : 0;
+    const int r = first_row + 32 * wave + col;
+    const int qi = r / p.group, qg = r - qi * p.group;
+    const bool live = qi < shown;
+    const int64_t row = q0 + qi;
+    const int hq = h * p.group + qg;
+    // last token that this lane's row sees; that all rows of the wave see; tokens that concern the workgroup
+    const int last = !live ? -1 : p.causal ? (int)(ctx - nq + qi) : ctx - 1;
+    const int all_last = (int)max((int64_t)-1, p.causal ? ctx - nq + (first_row + 32 * wave) / p.group : (int64_t)ctx - 1);
+    const int wave_last_q = min((first_row + 32 * wave + 31) / p.group, shown - 1);
+    const int wave_last = (first_row + 32 * wave) / p.group >= shown ? -1
+                          : p.causal ? (int)max((int64_t)-1, ctx - nq + wave_last_q) : ctx - 1;   // that any row of the wave sees
+    const int qi_last = min((first_row + kRowsWg - 1) / p.group, shown - 1);
+    const int end = (int)max((int64_t)0, p.causal ? ctx - nq + qi_last + 1 : (int64_t)ctx);
+    const int64_t lo = (int64_t)split * p.chunk;
+    const int begin = (int)min(lo, (int64_t)end), stop = (int)min(lo + p.chunk, (int64_t)end);
+    const float scale2 = fabsf(p.scale2);
+    const uint32_t record = (uint32_t)p.record;
+    const int32_t* table = p.block_table + (int64_t)b * p.table_width;
+    const int page_mask = (1 << p.page_shift) - 1;
+    int32_t* const slots = reinterpret_cast<int32_t*>(lds + 2 * M::kBytes);
+    uint32_t* const nan_flag = reinterpret_cast<uint32_t*>(lds + 2 * M::kBytes + kSlots * 4);   // some value is NaN
+
+    // What this thread moves of a tile.
+    v4u kreg[M::kKPer];
+    uint32_t vreg[M::kVPer][4], vsreg[M::kVPer][4];
+    Codes<D / 32> sreg;
+    uint32_t vthere[M::kVPer];
+    auto fetch = [&](int t_lds) {
+#pragma unroll
+        for (int c = 0; c < M::kKPer; ++c) {
+            const int i = threadIdx.x + c * M::kThreads;
+            if (M::kKLoads >= M::kThreads || i < M::kKLoads) {
+                const uint32_t slot = (uint32_t)max(slots[t_lds + i / (D / 32)], 0);
+                kreg[c] = load16(p.cache + (uint64_t)slot * record + (uint32_t)(h * (D / 2) + (i % (D / 32)) * 16));
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < M::kVPer; ++c) {
+            const int i = threadIdx.x + c * M::kThreads;
+            if (M::kVLoads >= M::kThreads || i < M::kVLoads) {
+                const int tg4 = i / (D / 8), dg = i % (D / 8);
+                const int4 s4 = *reinterpret_cast<const int4*>(slots + t_lds + 4 * tg4);
+                const int ss[4] = {s4.x, s4.y, s4.z, s4.w};
+                vthere[c] = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint8_t* rec = p.cache + (uint64_t)(uint32_t)max(ss[j], 0) * record;
+                    const uint32_t w = *reinterpret_cast<const uint32_t*>(rec + (uint32_t)((p.kv_heads + h) * (D / 2) + dg * 4));
+                    const uint32_t e = rec[(uint32_t)(p.kv_heads * D + (p.kv_heads + h) * (D / 32) + dg / 4)];
+                    vreg[c][j] = w;
+                    vsreg[c][j] = e;
+                    vthere[c] |= ss[j] >= 0 ? 1u << j : 0u;
+                }
+            }
+        }
+        if (threadIdx.x < M::kSLoads) {
+            const int v = threadIdx.x / M::kTile;
+            const uint32_t slot = (uint32_t)max(slots[t_lds + threadIdx.x % M::kTile], 0);
+            sreg = load_codes<D / 32>(p.cache + (uint64_t)slot * record +
+                                      (uint32_t)(p.kv_heads * D + (v * p.kv_heads + h) * (D / 32)));
+        }
+    };
+    auto stage = [&](int buf) {
+        uint8_t* base = lds + buf * M::kBytes;
+#pragma unroll
+        for (int c = 0; c < M::kKPer; ++c) {
+            const int i = threadIdx.x + c * M::kThreads;
+            if (M::kKLoads >= M::kThreads || i < M::kKLoads)
+                *reinterpret_cast<v4u*>(base + mk_place<D>(i / (D / 32), i % (D / 32))) = kreg[c];
+        }
+        bool bad = false;
+#pragma unroll
+        for (int c = 0; c < M::kVPer; ++c) {
+            const int i = threadIdx.x + c * M::kThreads;
+            if (M::kVLoads >= M::kThreads || i < M::kVLoads) {
+                const int tg4 = i / (D / 8), dg = i % (D / 8);
+                // four tokens from 4 tg4: half-chunk (tg4 >> 1) & 1 of chunk 2 s + half
+                const int chunk = (tg4 >> 3) * 4 + ((tg4 >> 2) & 1) * 2 + (tg4 & 1), upper = (tg4 >> 1) & 1;
+                float sc[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    // tokens that are not there, and NaN blocks (their rows get NaN in `use`), are zeros
+                    const bool here = (vthere[c] >> j) & 1, nan = vsreg[c][j] == 255u;
+                    bad |= here && nan;
+                    if (!here || nan) vreg[c][j] = 0u, vsreg[c][j] = 127u;
+                    sc[j] = scale_of(vsreg[c][j]);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t u[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) u[j] = unpack<E>(vreg[c][j], sc[j], k);
+                    uint8_t* at = base + M::kK + upper * 8;
+                    *reinterpret_cast<v2u*>(at + mv_place<M::kTile>(8 * dg + 2 * k, chunk)) =
+                        v2u{__builtin_amdgcn_perm(u[1], u[0], 0x05040100u), __builtin_amdgcn_perm(u[3], u[2], 0x05040100u)};
+                    *reinterpret_cast<v2u*>(at + mv_place<M::kTile>(8 * dg + 2 * k + 1, chunk)) =
+                        v2u{__builtin_amdgcn_perm(u[1], u[0], 0x07060302u), __builtin_amdgcn_perm(u[3], u[2], 0x07060302u)};
+                }
+            }
+        }
+        if (bad) *nan_flag = 1u;
+        if (threadIdx.x < M::kSLoads) {
+            uint8_t* at = base + M::kK + M::kV + threadIdx.x * (D / 32);
+            if constexpr (D == 64)
+                *reinterpret_cast<uint16_t*>(at) = (uint16_t)sreg.w[0];
+            else if constexpr (D == 128)
+                *reinterpret_cast<uint32_t*>(at) = sreg.w[0];
+            else
+                *reinterpret_cast<v2u*>(at) = v2u{sreg.w[0], sreg.w[1]};
+        }
+    };
+
+    // Queries: of dimensions 64 c + 16 half + (0 .. 15) and 32 more, per term.
+    v8i qf[kRuns][kTerms];
+    uint32_t qs[kRuns];   // scale of dimensions 64 c + 32 half ..
+    auto load_queries = [&]() {
+        const E* q = live ? static_cast<const E*>(p.q) + row * p.qt + hq * p.qh : nullptr;
+        const float sign = p.scale2 < 0.f ? -1.f : 1.f;
+#pragma unroll
+        for (int c = 0; c < kRuns; ++c) {
+            float x[2][16];
+            uint32_t m[2] = {0, 0};
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    x8 v = {};
+                    if (q) v = *reinterpret_cast<const x8*>(q + 64 * c + 32 * g + 16 * half + 8 * i);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        x[g][8 * i + j] = (float)v[j];
+                        m[g] = max(m[g], __float_as_uint((float)v[j]) & 0x7FFFFFFFu);
+                    }
+                }
+            uint32_t byte[2];
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                m[g] = max(m[g], (uint32_t)__shfl_xor((int)m[g], 32, 64));
+                const int e = (int)(m[g] >> 23);
+                byte[g] = e == 255 ? 255u : (uint32_t)max(e - 7, 16);
+                const float inv = e == 255 ? 0.f : __uint_as_float((254u - byte[g]) << 23) * sign;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[g][i] = e == 255 ? 0.f : x[g][i] * inv;
+            }
+            qs[c] = half ? byte[1] : byte[0];
+#pragma unroll
+            for (int t = 0; t < kTerms; ++t) {
+                split16(x[0], qf[c][t], 0);
+                split16(x[1], qf[c][t], 4);
+            }
+        }
+    };
+
+    float m = -INFINITY, limit = -INFINITY, base = 0.f, sum = 0.f;
+    v16f o[kDt];
+#pragma unroll
+    for (int n = 0; n < kDt; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[n][i] = 0.f;
+
+    uint32_t nan_blocks = 0;   // bit n: the row sees a value that is NaN in dimensions 32 n ..
+    // Where the lane reads K (token col) and V (dimension col): what varies is
+    // added or, inside a turned row, flipped.
+    const int k_row = mk_place<D>(col, half);
+    const int v_row = col * (2 * M::kTile), v_turn = mv_place<M::kTile>(col, half) - v_row;
+    // 32 tokens from t0, at token `tok` of the tile in `buf`.
+    auto use = [&](int buf, int tok, int t0, uint32_t there) {
+        const uint8_t* kb = lds + buf * M::kBytes;
+        const uint8_t* vb = kb + M::kK;
+        const uint8_t* sb = vb + M::kV + (tok + col) * (D / 32);
+        v16f sc;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < kRuns; ++c) {
+            const v4u k = *reinterpret_cast<const v4u*>(kb + tok * (D / 2) + (k_row ^ (32 * c)));
+            const uint32_t ks = sb[2 * c + half];
+#pragma unroll
+            for (int t = kTerms - 1; t >= 0; --t)
+                sc = mfma_mx32(k, ks, qf[c][t], qs[c] == 255 ? 255u : qs[c] - 4u * t, sc);
+        }
+        const bool full = there == 0xFFFFFFFFu && t0 + 31 <= all_last;   // wave-uniform
+        uint32_t seen = 0;   // bit i: this row sees token 8 (i / 4) + 4 half + i % 4
+        if (!full) {
+            int half_now = half;
+            asm("" : "+v"(half_now));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int n = 8 * (i >> 2) + 4 * half_now + (i & 3);
+                const bool see = ((there >> n) & 1) && t0 + n <= last;
+                seen |= see ? 1u << i : 0u;
+                if (!see) sc[i] = -INFINITY;
+            }
+        }
+        float top = max3(sc[0], sc[1], sc[2]);
+#pragma unroll
+        for (int i = 3; i < 15; i += 2) top = max3(top, sc[i], sc[i + 1]);
+        top = max2(top, sc[15]);
+        if (__any(top > limit)) {
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float m_new = fmaxf(m, top);
+            const float keep = m_new == m || m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m_new) * scale2);
+            m = m_new;
+            base = m == -INFINITY ? 0.f : m * scale2;
+            limit = scale2 > 0.f ? m + 8.f / scale2 : m;
+            sum *= keep;
+#pragma unroll
+            for (int n = 0; n < kDt; ++n) o[n] *= keep;
+        }
+        float w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], scale2, -base));
+        if (!full) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = (seen >> i) & 1 ? w[i] : 0.f;
+        }
+        float part[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[i] = (w[4 * i] + w[4 * i + 1]) + (w[4 * i + 2] + w[4 * i + 3]);
+        sum += (part[0] + part[1]) + (part[2] + part[3]);
+        v4u pf[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) pf[s][j] = pack2<E>(w[8 * s + 2 * j], w[8 * s + 2 * j + 1]);
+        if (__builtin_amdgcn_readfirstlane(*nan_flag)) {
+            // Some value block so far is NaN. Its codes were taken as zeros,
+            // because a row that does not see it has weight zero, and NaN times
+            // zero is not; the rows that see it remember its dimensions.
+            const uint8_t* vsb = vb + M::kV + M::kS + tok * (D / 32);
+#pragma unroll 1
+            for (int t = 0; t < 32; ++t) {
+                uint32_t nan = 0;
+#pragma unroll
+                for (int n = 0; n < D / 32; ++n) nan |= vsb[t * (D / 32) + n] == 255 ? 1u << n : 0u;
+                nan_blocks |= ((there >> t) & 1) != 0 && t0 + t <= last ? nan : 0u;
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int n = 0; n < kDt; ++n) {
+                const v4u a = *reinterpret_cast<const v4u*>(vb + v_row + n * (64 * M::kTile) + ((v_turn ^ (2 * tok)) ^ (32 * ((n ^ s) & 3))));
+                o[n] = mfma32<E>(a, pf[s], o[n]);
+            }
+    };
+
+    if (threadIdx.x == 0) *nan_flag = 0u;
+    for (int piece = begin; piece < stop; piece += kSlots) {
+        const int fill = min(stop - piece, kSlots), padded = (fill + M::kTile - 1) / M::kTile * M::kTile;
+        lds_barrier();
+        for (int i = threadIdx.x; i < padded; i += M::kThreads) {
+            int slot = -1;
+            if (i < fill) {
+                const int page = table[(piece + i) >> p.page_shift];
+                if ((uint32_t)page < (uint32_t)p.pages) slot = (page << p.page_shift) + ((piece + i) & page_mask);
+            }
+            slots[i] = slot;
+        }
+        lds_barrier();
+        fetch(0);
+        if (piece == begin) load_queries();
+        stage(0);
+        fetch(min(M::kTile, padded - M::kTile));
+        lds_barrier();
+        int buf = 0;
+        for (int t = 0; t < padded; t += M::kTile) {
+            stage(buf ^ 1);
+            fetch(min(t + 2 * M::kTile, padded - M::kTile));
+#pragma unroll 1
+            for (int s = 0; s < M::kTile; s += 32) {
+                const int t0 = piece + t + s;
+                if (t0 > wave_last) break;
+                const uint32_t there = (uint32_t)__ballot(slots[t + s + col] >= 0);
+                use(buf, s, t0, there);
+            }
+            lds_barrier();
+            buf ^= 1;
+        }
+    }
+    sum += __shfl_xor(sum, 32, 64);
+    if (!live) return;
+    if (nan_blocks) {
+#pragma unroll
+        for (int n = 0; n < kDt; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[n][i] += (nan_blocks >> n) & 1 ? __builtin_nanf("") : 0.f;
+    }
+    const int64_t at = row * p.q_heads + hq;
+    const float m2 = m == -INFINITY ? m : m * scale2;
+    // lane: row col, dimensions 32 n + 8 b + 4 half + (0 .. 3)
+    if (p.splits > 1) {
+        const int64_t part = at * p.splits + split;
+        if (half == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * part) = float2{m2, sum};
+        if (sum == 0.f) return;
+        float* po = p.part_o + part * D + 4 * half;
+#pragma unroll
+        for (int n = 0; n < kDt; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<v4f*>(po + 32 * n + 8 * g) = v4f{o[n][4 * g], o[n][4 * g + 1], o[n][4 * g + 2], o[n][4 * g + 3]};
+        return;
+    }
+    const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;   // NaN stays
+    if (p.lse && half == 0) p.lse[at] = sum == 0.f ? -INFINITY : (m2 + log2f(sum)) * kLn2;
+    uint16_t* out = static_cast<uint16_t*>(p.out) + at * D + 4 * half;
+#pragma unroll
+    for (int n = 0; n < kDt; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<v2u*>(out + 32 * n + 8 * g) = v2u{pack2<E>(o[n][4 * g] * inv, o[n][4 * g + 1] * inv),
+                                                             pack2<E>(o[n][4 * g + 2] * inv, o[n][4 * g + 3] * inv)};
 }
 
 // One workgroup per served query row and head: its splits joined in a fixed
@@ -685,10 +1074,16 @@ __global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
 
 template <class E, int D>
 gvr_status launch(const AttnParams& p, void* stream) {
+    if (p.many) {
+        typedef Many<D, D == 256 ? 4 : 8> M;
+        hipLaunchKernelGGL((many_rows_kernel<E, D, D == 256 ? 4 : 8>), dim3((unsigned)p.jobs), dim3(M::kThreads), M::kLds,
+                           (hipStream_t)stream, p);
+    } else {
     const int join = p.tw_shift ? gvr_kv4::kWaves / 2 * (D / 16 * 1024 + 512) : 0;   // bytes of the waves' join
     const int queries = (Query<E, D>::kRuns * Query<E, D>::kPer * 2048) << p.hw_shift;
     hipLaunchKernelGGL((few_rows_kernel<E, D>), dim3((unsigned)p.jobs), dim3(kThreads), max(join, WaveLds<D>::kLds + queries),
                        (hipStream_t)stream, p);
+    }
     if (hipGetLastError() != hipSuccess) return GVR_ERR_HIP;
     if (p.splits > 1) {
         hipLaunchKernelGGL((combine_kernel<E, D>), dim3((unsigned)((int64_t)p.sequences * p.max_q * p.q_heads)), dim3(256),
@@ -744,6 +1139,7 @@ gvr_status gvr_kv4_attention(const gvr_kv4_cache* cache, const gvr_kv4_attention
     p.sequences = a.sequences;
     p.uniform_q = a.q_start ? 0 : (int32_t)(a.T / a.sequences);
     p.max_q = plan.max_q, p.tiles = plan.tiles, p.jobs = plan.jobs, p.splits = plan.splits, p.chunk = plan.chunk;
+    p.many = plan.many;
     p.hw_shift = plan.hw_shift, p.tw_shift = plan.tw_shift;
     p.K = a.K, p.causal = a.causal;
     p.scale2 = a.scale * kLog2e;

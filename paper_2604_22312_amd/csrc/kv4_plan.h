@@ -57,10 +57,12 @@ constexpr int kSlots = 4096;       // tokens whose slots a workgroup holds in LD
 constexpr int kMaxSplits = 1024;
 constexpr int kCus = 256;          // compute units, each with one workgroup at a time (D = 64: two)
 constexpr int kMinTiles = 4;       // fewest tiles of a workgroup worth another split
+constexpr int kFewRows = 48;       // query rows of a KV head up to which the few-rows kernel serves
 constexpr int kShort = 64;         // steps of a context that one workgroup takes, so that no second kernel runs
 
 struct AttnPlan {
     int max_q;        // query tokens of a sequence
+    bool many;        // the kernel for many query rows
     int tiles;        // row tiles of a sequence and KV head
     int hw_shift;     // log2 of the KV heads of a workgroup
     int tw_shift;     // log2 of the waves that share a head's steps
@@ -79,12 +81,33 @@ inline AttnPlan plan_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_a
     const int G = a.q_heads / c.kv_heads;
     p.max_q = a.q_start ? a.max_q : (int)(a.T / a.sequences);
     if (p.max_q > a.T) p.max_q = (int)a.T;
-    const int64_t tiles = a.selection ? (int64_t)p.max_q * ((G + kRows - 1) / kRows)
+    // Many rows of a KV head that see (nearly) the same tokens: V is unpacked
+    // once for all of them.
+    p.many = !a.selection && (int64_t)p.max_q * G > kFewRows;
+    const int rows_wg = c.head_dim == 256 ? 128 : 256;
+    const int64_t tiles = p.many ? ((int64_t)p.max_q * G + rows_wg - 1) / rows_wg : a.selection ? (int64_t)p.max_q * ((G + kRows - 1) / kRows)
                                       : ((int64_t)p.max_q * G + kRows - 1) / kRows;
     p.tiles = (int)(tiles > kMaxCount ? kMaxCount : tiles);
     const int64_t n = a.selection ? a.K : a.table_width * c.page_size;
     const int64_t steps = (n + kStep - 1) / kStep;
     const int64_t units = (int64_t)a.sequences * tiles;
+    if (p.many) {
+        p.hw_shift = p.tw_shift = 0;
+        const int64_t unit = rows_wg / 2, wgs = units * c.kv_heads;
+        int64_t splits = wgs > 0 && wgs < kCus ? kCus / wgs : 1;
+        const int64_t most = (n + 4 * unit - 1) / (4 * unit);   // four tiles at least
+        splits = splits > most ? most : splits;
+        if (splits < 1) splits = 1;
+        while (splits > 1 && partial_bytes(a.T, a.q_heads, c.head_dim, splits) > ws_bytes) --splits;
+        int64_t chunk = ((n + splits - 1) / splits + unit - 1) / unit * unit;
+        if (chunk < unit) chunk = unit;
+        splits = n > 0 ? (n + chunk - 1) / chunk : 1;
+        p.chunk = (int)(chunk > kMaxCount ? kMaxCount / unit * unit : chunk);
+        p.splits = (int)splits;
+        p.jobs = wgs * splits;
+        p.ws_bytes = partial_bytes(a.T, a.q_heads, c.head_dim, splits);
+        return p;
+    }
     // KV heads of a workgroup: all that divide evenly (a record's parts are then
     // read together), fewer, with more waves to each, while that spares splits
     // and the contexts still last for several tiles.
