@@ -37,7 +37,9 @@
 #include <stdint.h>
 
 #include "gvr_kv4.h"
+#pragma clang force_cuda_host_device begin
 #include "kv4_plan.h"
+#pragma clang force_cuda_host_device end
 #include "wave_ops.h"
 
 namespace {
@@ -73,7 +75,7 @@ struct AttnParams {
     int64_t table_width, record, T, jobs;
     int32_t page_shift, kv_heads, q_heads, group, sequences, uniform_q, max_q, tiles, splits, chunk, K, causal;
     int32_t pages;
-    int32_t many;
+    int32_t many, row_tiles;      // the many-rows kernel, or the few-rows one with so many tiles of 16 rows a wave
     int32_t hw_shift, tw_shift;   // log2 of a workgroup's KV heads, and of the waves that share a head's steps
     float scale2;     // scale * log2(e)
 };
@@ -279,8 +281,24 @@ DEV void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <class E, int D>
-__global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(AttnParams p) {
+// The work of a workgroup: unit u of U (a sequence's split) and one of `inner`
+// jobs of the unit. Jobs of a unit read the same records, so they go to one
+// XCD (workgroups are dealt to the eight in turn), where they meet in its L2.
+struct Job {
+    int64_t unit;
+    int inner;
+};
+DEV Job job_of(uint32_t bid, int64_t units, int inner) {
+    if (gvr_kv4::by_xcd(units)) {
+        const uint32_t y = bid >> 3;
+        return {(int64_t)(y / (uint32_t)inner) * 8 + (bid & 7), (int)(y % (uint32_t)inner)};
+    }
+    return {bid / (uint32_t)inner, (int)(bid % (uint32_t)inner)};
+}
+
+// MT: row tiles of 16 that a wave serves with one pass over K and V.
+template <class E, int D, int MT>
+__global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16) ? 4 : 2) void few_rows_kernel(AttnParams p) {
     constexpr int NT = D / 16;        // dimensions of V per lane = matrix steps of the second product
     typedef Query<E, D> Q;
     typedef WaveLds<D> L;
@@ -290,14 +308,12 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
     const int hl = wave & ((1 << p.hw_shift) - 1);        // head of the workgroup's
     const int tg = wave >> p.hw_shift;                    // part of the tile's tokens
     const int tt_shift = 5 + p.tw_shift, TT = 1 << tt_shift;   // tokens of a tile
-    uint32_t job = blockIdx.x;
     const int groups = p.kv_heads >> p.hw_shift;
-    const int h0 = (int)(job % (uint32_t)groups) << p.hw_shift, h = h0 + hl;
-    job /= (uint32_t)groups;
-    const int tile = (int)(job % (uint32_t)p.tiles);
-    job /= (uint32_t)p.tiles;
-    const int split = (int)(job % (uint32_t)p.splits);
-    const int b = (int)(job / (uint32_t)p.splits);
+    const int64_t units = (int64_t)p.sequences * p.splits;
+    const Job job = job_of(blockIdx.x, units, groups * p.tiles);
+    if (job.unit >= units) return;
+    const int h = (job.inner % groups << p.hw_shift) + hl, tile = job.inner / groups;
+    const int b = (int)(job.unit / p.splits), split = (int)(job.unit % p.splits);
 
     const Rows rows = rows_of(p, b);
     const int64_t q0 = rows.q0, nq = rows.nq;
@@ -306,39 +322,47 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
     const int64_t held = p.table_width << p.page_shift;
     const int ctx = p.pages > 0 ? (int)min((int64_t)max(p.ctx_len[b], 0), held) : 0;
 
-    // this lane's query row; tokens [0, end) of the context or selection concern the tile
-    int qi, qg, end, sel_last = 0;
-    bool live;
+    // this lane's query rows; tokens [0, end) of the context or selection concern the tile
+    int qi[MT], qg[MT], end, sel_last = 0;
+    bool live[MT];
     const int32_t* list = nullptr;
     if (p.selection) {
-        const int per = (p.group + kRows - 1) / kRows, token = tile / per;
+        const int per = (p.group + MT * kRows - 1) / (MT * kRows), token = tile / per;
         if (token >= shown) return;
-        qi = token;
-        qg = (tile - token * per) * kRows + col;
-        live = qg < p.group;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            qi[mt] = token;
+            qg[mt] = (tile - token * per) * (MT * kRows) + mt * kRows + col;
+            live[mt] = qg[mt] < p.group;
+        }
         end = p.pages > 0 ? p.K : 0;
         list = p.selection + (q0 + token) * p.K;
         sel_last = p.causal ? (int)(ctx - nq + token) : ctx - 1;
     } else {
-        const int r = tile * kRows + col;
-        qi = r / p.group;
-        qg = r - qi * p.group;
-        live = qi < shown;
-        if ((tile * kRows) / p.group >= shown) return;
-        const int qi_last = min((tile * kRows + kRows - 1) / p.group, shown - 1);
+        const int r0 = tile * (MT * kRows);
+        if (r0 / p.group >= shown) return;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int r = r0 + mt * kRows + col;
+            qi[mt] = r / p.group;
+            qg[mt] = r - qi[mt] * p.group;
+            live[mt] = qi[mt] < shown;
+        }
+        const int qi_last = min((r0 + MT * kRows - 1) / p.group, shown - 1);
         end = (int)max((int64_t)0, p.causal ? ctx - nq + qi_last + 1 : (int64_t)ctx);
     }
-    const int64_t row = q0 + qi;
-    const int hq = h * p.group + qg;
-    // last token that this lane's row sees, and the last that all of the tile's rows see
-    const int last = !live ? -1 : list ? 0x7FFFFFFF : p.causal ? (int)(ctx - nq + qi) : ctx - 1;
-    const int all_last = list ? 0x7FFFFFFF
-                              : (int)max((int64_t)-1, p.causal ? ctx - nq + (tile * kRows) / p.group : (int64_t)ctx - 1);
+    // last token that this lane's rows see, and the last that all of the tile's rows see
+    int last[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+        last[mt] = !live[mt] ? -1 : list ? 0x7FFFFFFF : p.causal ? (int)(ctx - nq + qi[mt]) : ctx - 1;
+    const int all_last =
+        list ? 0x7FFFFFFF
+             : (int)max((int64_t)-1, p.causal ? ctx - nq + (tile * (MT * kRows)) / p.group : (int64_t)ctx - 1);
     const int64_t lo = (int64_t)split * p.chunk;
     const int begin = (int)min(lo, (int64_t)end), stop = (int)min(lo + p.chunk, (int64_t)end);
 
     const float scale2 = fabsf(p.scale2);
-    const E* const q_row = live ? static_cast<const E*>(p.q) + row * p.qt + hq * p.qh : nullptr;
     const uint32_t record = (uint32_t)p.record;
     const int32_t* table = p.block_table + (int64_t)b * p.table_width;
     const int page_mask = (1 << p.page_shift) - 1;
@@ -353,12 +377,13 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
     const uint8_t* const s_src = p.cache + (uint32_t)(p.kv_heads * D + ((quarter & 1 ? p.kv_heads : 0) + h) * (D / 32));
     uint8_t* const mine = lds + wave * L::kBytes;
     int32_t* const slots = reinterpret_cast<int32_t*>(lds + gvr_kv4::kWaves * L::kBytes);
+    constexpr int kTerms = Q::kRuns * Q::kPer;
     // The head's queries stay in LDS (16 bytes a lane side by side): they are
     // needed once a step, and their registers are worth a second workgroup.
-    v4u* const q_lds = reinterpret_cast<v4u*>(lds + L::kLds) + hl * (Q::kRuns * Q::kPer * 2 * 64) + lane;
-    uint32_t q_scale[Q::kRuns * Q::kPer];
-    auto query = [&](int i) {
-        const v4u a = q_lds[i * 128], b = q_lds[i * 128 + 64];
+    v4u* const q_lds = reinterpret_cast<v4u*>(lds + L::kLds) + hl * (MT * kTerms * 2 * 64) + lane;
+    uint32_t q_scale[MT][kTerms];
+    auto query = [&](int mt, int i) {
+        const v4u a = q_lds[(mt * kTerms + i) * 128], b = q_lds[(mt * kTerms + i) * 128 + 64];
         return v8i{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
     };
     struct Step {
@@ -392,13 +417,20 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
         vr_at[i] = v_place<D>(4 * quarter + i, byte / 16) + byte % 16;
     }
 
-    float m = -INFINITY, limit = -INFINITY, base = 0.f, sum = 0.f;
-    // maximum (of unscaled scores) that the weights refer to, the score that moves it, maximum * scale2
-    v4f o[NT];
+    // Of each row: the maximum (of unscaled scores) that its weights refer to, the
+    // score that moves it, maximum * scale2, the sum; whether it sees a value that
+    // is NaN in this lane's dimensions (D = 256: lower, upper half).
+    float m[MT], limit[MT], base[MT], sum[MT];
+    uint32_t nan_blocks[MT];
+    v4f o[MT][NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) o[n] = v4f{0.f, 0.f, 0.f, 0.f};
-
-    uint32_t nan_blocks = 0;   // the row sees a value that is NaN in this lane's dimensions (D = 256: lower, upper half)
+    for (int mt = 0; mt < MT; ++mt) {
+        m[mt] = limit[mt] = -INFINITY;
+        base[mt] = sum[mt] = 0.f;
+        nan_blocks[mt] = 0;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[mt][n] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
     // t0: first token (or place in the list) of the step; its registers take
     // the step at slot t_next when they are free.
     auto use = [&](Step& d, int t0, int t_next) {
@@ -416,14 +448,20 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
             else
                 *reinterpret_cast<v2u*>(sw) = v2u{d.s[t].w[0], d.s[t].w[1]};
         }
-        v4f sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        // the wave's lanes read what other lanes wrote (in order, without a barrier)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+        v4f sc[MT][2];
 #pragma unroll
-        for (int i = Q::kRuns * Q::kPer - 1; i >= 0; --i) {   // (D = 64: runs of the same K; else terms, then runs of K)
-            const int c = D == 64 ? 0 : i / Q::kPer;
-            const v8i qi8 = query(i);
+        for (int mt = 0; mt < MT; ++mt) {
+            sc[mt][0] = sc[mt][1] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-                sc[t] = mfma_mx(d.k[t][c], mine[ks_at + 16 * t * (D / 32) + 4 * c], qi8, q_scale[i], sc[t]);
+            for (int i = kTerms - 1; i >= 0; --i) {   // (D = 64: runs of the same K; else terms, then runs of K)
+                const int c = D == 64 ? 0 : i / Q::kPer;
+                const v8i qf = query(mt, i);
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    sc[mt][t] = mfma_mx(d.k[t][c], mine[ks_at + 16 * t * (D / 32) + 4 * c], qf, q_scale[mt][i], sc[mt][t]);
+            }
         }
         fetch(t_next, d);
         Codes<D / 32> v[8];
@@ -444,44 +482,12 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
         const bool full = there == 0xFFFFFFFFu && t0 + kStep - 1 <= all_last;   // wave-uniform
         int quarter_now = quarter;   // (its multiples are not worth registers through the loop)
         asm("" : "+v"(quarter_now));
-        uint32_t seen = 0xFFu;   // bit 4 t + i: this row sees token 16 t + 4 quarter + i
+        v4u pf[MT];
+        bool bad = false;
         if (!full) {
-            seen = 0;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int n = 16 * t + 4 * quarter_now + i;
-                    const bool see = ((there >> n) & 1) && t0 + n <= last;
-                    seen |= see ? 1u << (4 * t + i) : 0u;
-                    if (!see) sc[t][i] = -INFINITY;
-                }
-        }
-        float top = max2(max3(max3(sc[0][0], sc[0][1], sc[0][2]), sc[0][3], sc[1][0]),
-                         max3(sc[1][1], sc[1][2], sc[1][3]));
-        if (__any(top > limit)) {
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float m_new = fmaxf(m, top);
-            // (nothing seen so far: sum and O are zero)
-            const float keep = m_new == m || m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m_new) * scale2);
-            m = m_new;
-            base = m == -INFINITY ? 0.f : m * scale2;
-            limit = scale2 > 0.f ? m + 8.f / scale2 : m;
-            sum *= keep;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) o[n] *= keep;
-        }
-        float w[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j >> 2][j & 3], scale2, -base));
-        if (!full) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = (seen >> j) & 1 ? w[j] : 0.f;
             // A masked token's weight is zero, but a NaN block times zero is
             // not: blocks that are NaN, and tokens that are not there, are
             // taken as zeros, and the rows that see a NaN remember it.
-            bool bad = false;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const bool here = (there >> (16 * (j >> 2) + 4 * quarter_now + (j & 3))) & 1;
@@ -499,12 +505,52 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
                 for (int n = 0; n < kStep; ++n) {
                     uint32_t nan = vsb[n * (D / 32)] == 255 ? 1u : 0u;
                     if constexpr (D == 256) nan |= vsb[n * (D / 32) + 1] == 255 ? 2u : 0u;
-                    nan_blocks |= ((there >> n) & 1) != 0 && t0 + n <= last ? nan : 0u;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+                        nan_blocks[mt] |= ((there >> n) & 1) != 0 && t0 + n <= last[mt] ? nan : 0u;
                 }
             }
         }
-        sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-        const v4u pf = {pack2<E>(w[0], w[1]), pack2<E>(w[2], w[3]), pack2<E>(w[4], w[5]), pack2<E>(w[6], w[7])};
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            v4f(&s)[2] = sc[mt];
+            uint32_t seen = 0;   // bit 4 t + i: this row sees token 16 t + 4 quarter + i
+            if (!full) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int n = 16 * t + 4 * quarter_now + i;
+                        const bool see = ((there >> n) & 1) && t0 + n <= last[mt];
+                        seen |= see ? 1u << (4 * t + i) : 0u;
+                        if (!see) s[t][i] = -INFINITY;
+                    }
+            }
+            float top = max2(max3(max3(s[0][0], s[0][1], s[0][2]), s[0][3], s[1][0]), max3(s[1][1], s[1][2], s[1][3]));
+            if (__any(top > limit[mt])) {
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float m_new = fmaxf(m[mt], top);
+                // (nothing seen so far: sum and O are zero)
+                const float keep =
+                    m_new == m[mt] || m[mt] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[mt] - m_new) * scale2);
+                m[mt] = m_new;
+                base[mt] = m_new == -INFINITY ? 0.f : m_new * scale2;
+                limit[mt] = scale2 > 0.f ? m_new + 8.f / scale2 : m_new;
+                sum[mt] *= keep;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) o[mt][n] *= keep;
+            }
+            float w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j >> 2][j & 3], scale2, -base[mt]));
+            if (!full) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = (seen >> j) & 1 ? w[j] : 0.f;
+            }
+            sum[mt] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+            pf[mt] = v4u{pack2<E>(w[0], w[1]), pack2<E>(w[2], w[3]), pack2<E>(w[4], w[5]), pack2<E>(w[6], w[7])};
+        }
 #pragma unroll
         for (int n = 0; n < NT; n += 2) {
             uint32_t u[8];
@@ -516,9 +562,13 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
                 a0[j] = __builtin_amdgcn_perm(u[2 * j + 1], u[2 * j], 0x05040100u);
                 a1[j] = __builtin_amdgcn_perm(u[2 * j + 1], u[2 * j], 0x07060302u);
             }
-            o[n] = mfma<E>(a0, pf, o[n]);
-            o[n + 1] = mfma<E>(a1, pf, o[n + 1]);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                o[mt][n] = mfma<E>(a0, pf[mt], o[mt][n]);
+                o[mt][n + 1] = mfma<E>(a1, pf[mt], o[mt][n + 1]);
+            }
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");   // the next step writes where this one read
     };
 
     // Pieces of the chunk: slots into LDS, then step after step, the loads two
@@ -544,14 +594,20 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
         Step d;
         fetch(first, d);
         if (piece == begin) {   // while the first loads run
-            const Q q = load_query<E, D>(q_row, p.scale2 < 0.f ? -1.f : 1.f, lane);
 #pragma unroll
-            for (int i = 0; i < Q::kRuns * Q::kPer; ++i) {
-                const v8i b = q.b[i / Q::kPer][i % Q::kPer];
-                q_scale[i] = q.scale[i / Q::kPer][i % Q::kPer];
-                if (tg == 0) {
-                    q_lds[i * 128] = v4u{(uint32_t)b[0], (uint32_t)b[1], (uint32_t)b[2], (uint32_t)b[3]};
-                    q_lds[i * 128 + 64] = v4u{(uint32_t)b[4], (uint32_t)b[5], (uint32_t)b[6], (uint32_t)b[7]};
+            for (int mt = 0; mt < MT; ++mt) {
+                const int64_t at = (q0 + qi[mt]) * p.qt + (h * p.group + qg[mt]) * p.qh;
+                const Q q = load_query<E, D>(live[mt] ? static_cast<const E*>(p.q) + at : nullptr,
+                                             p.scale2 < 0.f ? -1.f : 1.f, lane);
+#pragma unroll
+                for (int i = 0; i < kTerms; ++i) {
+                    const v8i b = q.b[i / Q::kPer][i % Q::kPer];
+                    q_scale[mt][i] = q.scale[i / Q::kPer][i % Q::kPer];
+                    if (tg == 0) {
+                        v4u* to = q_lds + (mt * kTerms + i) * 128;
+                        to[0] = v4u{(uint32_t)b[0], (uint32_t)b[1], (uint32_t)b[2], (uint32_t)b[3]};
+                        to[64] = v4u{(uint32_t)b[4], (uint32_t)b[5], (uint32_t)b[6], (uint32_t)b[7]};
+                    }
                 }
             }
             lds_barrier();
@@ -561,63 +617,78 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void few_rows_kernel(Att
             __builtin_amdgcn_s_barrier();
         }
     }
-    sum += __shfl_xor(sum, 16, 64);
-    sum += __shfl_xor(sum, 32, 64);
-    if (nan_blocks) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+    for (int mt = 0; mt < MT; ++mt) {
+        sum[mt] += __shfl_xor(sum[mt], 16, 64);
+        sum[mt] += __shfl_xor(sum[mt], 32, 64);
+        if (nan_blocks[mt]) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[n][i] += (nan_blocks >> (D == 256 ? i / 2 : 0)) & 1 ? __builtin_nanf("") : 0.f;
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    o[mt][n][i] += (nan_blocks[mt] >> (D == 256 ? i / 2 : 0)) & 1 ? __builtin_nanf("") : 0.f;
+        }
     }
 
     // Join the waves of a head: half of them hand theirs to the other half.
     for (int half = (1 << p.tw_shift) >> 1; half > 0; half >>= 1) {
         const int places = half << p.hw_shift;   // of waves in LDS
-        const int place = (tg & (half - 1)) << p.hw_shift | (wave & ((1 << p.hw_shift) - 1));
-        v4f* lo4 = reinterpret_cast<v4f*>(lds) + (place * NT) * 64 + lane;
-        float2* lml = reinterpret_cast<float2*>(lds + (size_t)places * NT * 1024) + place * 64 + lane;
-        __syncthreads();
+        const int place = (tg & (half - 1)) << p.hw_shift | hl;
+        v4f* lo4 = reinterpret_cast<v4f*>(lds) + (place * MT * NT) * 64 + lane;
+        float2* lml = reinterpret_cast<float2*>(lds + (size_t)places * MT * NT * 1024) + place * MT * 64 + lane;
+        lds_barrier();
         if (tg >= half && tg < 2 * half) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) lo4[n * 64] = o[n];
-            *lml = float2{m, sum};
-        }
-        __syncthreads();
-        if (tg < half) {
-            const float2 other = *lml;
-            const float m_new = fmaxf(m, other.x);
-            const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * scale2);
-            const float theirs = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((other.x - m_new) * scale2);
-            sum = sum * mine + other.y * theirs;
-            m = m_new;
+            for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) o[n] = o[n] * mine + lo4[n * 64] * theirs;
+                for (int n = 0; n < NT; ++n) lo4[(mt * NT + n) * 64] = o[mt][n];
+                lml[mt * 64] = float2{m[mt], sum[mt]};
+            }
+        }
+        lds_barrier();
+        if (tg < half) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const float2 other = lml[mt * 64];
+                const float m_new = fmaxf(m[mt], other.x);
+                const float mine_w = m[mt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[mt] - m_new) * scale2);
+                const float theirs = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((other.x - m_new) * scale2);
+                sum[mt] = sum[mt] * mine_w + other.y * theirs;
+                m[mt] = m_new;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) o[mt][n] = o[mt][n] * mine_w + lo4[(mt * NT + n) * 64] * theirs;
+            }
         }
     }
-    if (tg != 0 || !live) return;
-    // lane: row col, dimensions (4 quarter + i) * NT + n
-    const int64_t at = row * p.q_heads + hq;
-    const float m2 = m == -INFINITY ? m : m * scale2;
-    if (p.splits > 1) {
-        const int64_t part = at * p.splits + split;
-        if (quarter == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * part) = float2{m2, sum};
-        if (sum == 0.f) return;
-        float* po = p.part_o + part * D;
+    if (tg != 0) return;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        if (!live[mt]) continue;
+        // lane: row col, dimensions (4 quarter + i) * NT + n
+        const int64_t at = (q0 + qi[mt]) * p.q_heads + h * p.group + qg[mt];
+        const float m2 = m[mt] == -INFINITY ? m[mt] : m[mt] * scale2;
+        if (p.splits > 1) {
+            const int64_t part = at * p.splits + split;
+            if (quarter == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * part) = float2{m2, sum[mt]};
+            if (sum[mt] == 0.f) continue;
+            float* po = p.part_o + part * D;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; n += 4)
+                    *reinterpret_cast<v4f*>(po + (4 * quarter + i) * NT + n) =
+                        v4f{o[mt][n][i], o[mt][n + 1][i], o[mt][n + 2][i], o[mt][n + 3][i]};
+            continue;
+        }
+        const float inv = sum[mt] > 0.f ? 1.f / sum[mt] : sum[mt] == 0.f ? 0.f : sum[mt];   // NaN stays
+        if (p.lse && quarter == 0) p.lse[at] = sum[mt] == 0.f ? -INFINITY : (m2 + log2f(sum[mt])) * kLn2;
+        uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at * D);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int n = 0; n < NT; n += 4)
-                *reinterpret_cast<v4f*>(po + (4 * quarter + i) * NT + n) = v4f{o[n][i], o[n + 1][i], o[n + 2][i], o[n + 3][i]};
-        return;
+            for (int n = 0; n < NT; n += 2)
+                out[((4 * quarter + i) * NT + n) / 2] = pack2<E>(o[mt][n][i] * inv, o[mt][n + 1][i] * inv);
     }
-    const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;   // NaN stays
-    if (p.lse && quarter == 0) p.lse[at] = sum == 0.f ? -INFINITY : (m2 + log2f(sum)) * kLn2;
-    uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at * D);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int n = 0; n < NT; n += 2)
-            out[((4 * quarter + i) * NT + n) / 2] = pack2<E>(o[n][i] * inv, o[n + 1][i] * inv);
 }
 
 // ---- many query rows
@@ -678,16 +749,13 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
     extern __shared__ __align__(16) uint8_t lds[];
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // Workgroups of one KV head are a multiple of kv_heads apart: with 8 heads
-    // each XCD's cache holds one head's context. The last rows, which see the
-    // longest context, come first.
-    uint32_t job = blockIdx.x;
-    const int h = (int)(job % (uint32_t)p.kv_heads);
-    job /= (uint32_t)p.kv_heads;
-    const int split = (int)(job % (uint32_t)p.splits);
-    job /= (uint32_t)p.splits;
-    const int b = (int)(job % (uint32_t)p.sequences);
-    const int tile = p.tiles - 1 - (int)(job / (uint32_t)p.sequences);
+    // The last rows, which see the longest context, come first.
+    const int64_t units = (int64_t)p.sequences * p.kv_heads * p.splits;
+    const Job job = job_of(blockIdx.x, units, p.tiles);
+    if (job.unit >= units) return;
+    const int tile = p.tiles - 1 - job.inner;
+    const int split = (int)(job.unit % p.splits), h = (int)(job.unit / p.splits % p.kv_heads);
+    const int b = (int)(job.unit / p.splits / p.kv_heads);
 
     const Rows rows = rows_of(p, b);
     const int64_t q0 = rows.q0, nq = rows.nq;
@@ -1079,10 +1147,17 @@ gvr_status launch(const AttnParams& p, void* stream) {
         hipLaunchKernelGGL((many_rows_kernel<E, D, D == 256 ? 4 : 8>), dim3((unsigned)p.jobs), dim3(M::kThreads), M::kLds,
                            (hipStream_t)stream, p);
     } else {
-    const int join = p.tw_shift ? gvr_kv4::kWaves / 2 * (D / 16 * 1024 + 512) : 0;   // bytes of the waves' join
-    const int queries = (Query<E, D>::kRuns * Query<E, D>::kPer * 2048) << p.hw_shift;
-    hipLaunchKernelGGL((few_rows_kernel<E, D>), dim3((unsigned)p.jobs), dim3(kThreads), max(join, WaveLds<D>::kLds + queries),
-                       (hipStream_t)stream, p);
+        const int rows = p.row_tiles;
+        const int join = p.tw_shift ? gvr_kv4::kWaves / 2 * rows * (D / 16 * 1024 + 512) : 0;   // bytes of the waves' join
+        const int queries = (rows * Query<E, D>::kRuns * Query<E, D>::kPer * 2048) << p.hw_shift;
+        const int lds = max(join, WaveLds<D>::kLds + queries);
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)p.jobs), dim3(kThreads), lds, (hipStream_t)stream, p);
+        };
+        if constexpr (D != 256)
+            rows == 2 ? go(few_rows_kernel<E, D, 2>) : go(few_rows_kernel<E, D, 1>);
+        else
+            go(few_rows_kernel<E, D, 1>);
     }
     if (hipGetLastError() != hipSuccess) return GVR_ERR_HIP;
     if (p.splits > 1) {
@@ -1139,7 +1214,7 @@ gvr_status gvr_kv4_attention(const gvr_kv4_cache* cache, const gvr_kv4_attention
     p.sequences = a.sequences;
     p.uniform_q = a.q_start ? 0 : (int32_t)(a.T / a.sequences);
     p.max_q = plan.max_q, p.tiles = plan.tiles, p.jobs = plan.jobs, p.splits = plan.splits, p.chunk = plan.chunk;
-    p.many = plan.many;
+    p.many = plan.many, p.row_tiles = plan.row_tiles;
     p.hw_shift = plan.hw_shift, p.tw_shift = plan.tw_shift;
     p.K = a.K, p.causal = a.causal;
     p.scale2 = a.scale * kLog2e;

@@ -57,13 +57,19 @@ constexpr int kSlots = 4096;       // tokens whose slots a workgroup holds in LD
 constexpr int kMaxSplits = 1024;
 constexpr int kCus = 256;          // compute units, each with one workgroup at a time (D = 64: two)
 constexpr int kMinTiles = 4;       // fewest tiles of a workgroup worth another split
-constexpr int kFewRows = 48;       // query rows of a KV head up to which the few-rows kernel serves
+constexpr int kFewRows = 64;       // query rows of a KV head up to which the few-rows kernel serves
 constexpr int kShort = 64;         // steps of a context that one workgroup takes, so that no second kernel runs
+
+// Whether units of workgroups that read the same records are dealt to the eight
+// XCDs: evenly, or so many that it comes to little.
+inline bool by_xcd(int64_t units) { return units % 8 == 0 || units >= 64; }
+inline int64_t grid_of(int64_t units, int64_t inner) { return (by_xcd(units) ? (units + 7) / 8 * 8 : units) * inner; }
 
 struct AttnPlan {
     int max_q;        // query tokens of a sequence
     bool many;        // the kernel for many query rows
-    int tiles;        // row tiles of a sequence and KV head
+    int row_tiles;    // few rows: tiles of kRows of a wave
+    int tiles;        // tiles of rows of a sequence and KV head (a workgroup's)
     int hw_shift;     // log2 of the KV heads of a workgroup
     int tw_shift;     // log2 of the waves that share a head's steps
     int64_t jobs;     // workgroups
@@ -85,8 +91,11 @@ inline AttnPlan plan_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_a
     // once for all of them.
     p.many = !a.selection && (int64_t)p.max_q * G > kFewRows;
     const int rows_wg = c.head_dim == 256 ? 128 : 256;
-    const int64_t tiles = p.many ? ((int64_t)p.max_q * G + rows_wg - 1) / rows_wg : a.selection ? (int64_t)p.max_q * ((G + kRows - 1) / kRows)
-                                      : ((int64_t)p.max_q * G + kRows - 1) / kRows;
+    // rows that share their tokens; two tiles a wave read K and V once for both
+    const int64_t together = a.selection ? G : (int64_t)p.max_q * G;
+    p.row_tiles = together > kRows && c.head_dim != 256 ? 2 : 1;
+    const int rows = p.many ? rows_wg : p.row_tiles * kRows;
+    const int64_t tiles = a.selection ? (int64_t)p.max_q * ((G + rows - 1) / rows) : (together + rows - 1) / rows;
     p.tiles = (int)(tiles > kMaxCount ? kMaxCount : tiles);
     const int64_t n = a.selection ? a.K : a.table_width * c.page_size;
     const int64_t steps = (n + kStep - 1) / kStep;
@@ -104,7 +113,7 @@ inline AttnPlan plan_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_a
         splits = n > 0 ? (n + chunk - 1) / chunk : 1;
         p.chunk = (int)(chunk > kMaxCount ? kMaxCount / unit * unit : chunk);
         p.splits = (int)splits;
-        p.jobs = wgs * splits;
+        p.jobs = grid_of((int64_t)a.sequences * c.kv_heads * splits, tiles);
         p.ws_bytes = partial_bytes(a.T, a.q_heads, c.head_dim, splits);
         return p;
     }
@@ -136,7 +145,7 @@ inline AttnPlan plan_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_a
     splits = n > 0 ? (n + chunk - 1) / chunk : 1;
     p.chunk = (int)(chunk > kMaxCount ? kMaxCount / unit * unit : chunk);
     p.splits = (int)splits;
-    p.jobs = units * (c.kv_heads >> p.hw_shift) * splits;
+    p.jobs = grid_of((int64_t)a.sequences * splits, tiles * (c.kv_heads >> p.hw_shift));
     p.ws_bytes = partial_bytes(a.T, a.q_heads, c.head_dim, splits);
     return p;
 }
