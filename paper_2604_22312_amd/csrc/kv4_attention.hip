@@ -47,7 +47,6 @@ namespace {
 using gvr_kv4::kRows;
 using gvr_kv4::kStep;
 using gvr_kv4::kThreads;
-using gvr_kv4::kSlots;
 using gvr_kv4::kMaxSplits;
 
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -65,8 +64,11 @@ struct AttnParams {
     const void* q;
     void* out;
     float* lse;
-    float* part_o;    // [T][q_heads][splits][D]
-    float* part_ml;   // [T][q_heads][splits][2]: maximum (log2 domain), sum
+    // Partial results of unit u (a sequence's split), of its query token i and head hq, at
+    // (u * max_q + i) * q_heads + hq: O [D], and maximum (log2 domain) and sum.
+    float* part_o;
+    float* part_ml;
+    int2* units_of;   // balanced splits: [sequences] first unit and number of units
     const int32_t* block_table;
     const int32_t* ctx_len;
     const int32_t* q_start;
@@ -75,6 +77,7 @@ struct AttnParams {
     int64_t table_width, record, T, jobs;
     int32_t page_shift, kv_heads, q_heads, group, sequences, uniform_q, max_q, tiles, splits, chunk, K, causal;
     int32_t pages;
+    int32_t balanced, units;      // splits sized in the kernel so that the contexts' lengths fill `units`
     int32_t many, row_tiles;      // the many-rows kernel, or the few-rows one with so many tiles of 16 rows a wave
     int32_t hw_shift, tw_shift;   // log2 of a workgroup's KV heads, and of the waves that share a head's steps
     float scale2;     // scale * log2(e)
@@ -263,6 +266,7 @@ struct WaveLds {
     static constexpr int kCodes = kStep * D / 2;
     static constexpr int kScales = kStep * D / 32;     // of K, then as many of V
     static constexpr int kBytes = kCodes + 2 * kScales;
+    static constexpr int kSlots = D == 256 ? 4096 : 8192;   // tokens whose slots the workgroup holds
     static constexpr int kLds = gvr_kv4::kWaves * kBytes + kSlots * 4;   // and the queries of the workgroup's heads
 };
 
@@ -279,6 +283,60 @@ DEV void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// A workgroup's unit of the balanced splits: sequence b's split `split` of
+// `count`, chunk tokens each.
+struct Unit {
+    int b, split, count, first, chunk;   // first: unit of split 0; b < 0: none
+};
+DEV int context_of(const AttnParams& p, int b) {
+    const int64_t held = p.table_width << p.page_shift;
+    return p.pages > 0 ? (int)min((int64_t)max(p.ctx_len[b], 0), held) : 0;
+}
+// The sequences' contexts are cut into chunks of one length, the least of eight
+// candidates (one per wave) for which the chunks count no more than the units.
+// Candidate 7 always serves: with n sequences and u units, chunks of at least
+// total / (u - n) are at most u - n full ones and n parts.
+DEV Unit find_unit(const AttnParams& p, int u, int tt_shift, int32_t* lds) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = p.sequences;
+    const int mine = lane < n ? context_of(p, lane) : 0;
+    auto context = [&](int b0) { return b0 == 0 ? mine : b0 + lane < n ? context_of(p, b0 + lane) : 0; };
+    float total = 0.f;
+    for (int b0 = 0; b0 < n; b0 += 64) total += gvr_dev::wave_sum_f((float)context(b0));
+    const float least = total / (float)p.units * 0.999999f;
+    const float most = total * 1.00001f / (float)(p.units - n) + 1.f;   // (float32 sums: a margin)
+    auto length = [&](int k) {
+        const float c = least + (most - least) * (float)k * (1.f / (gvr_kv4::kWaves - 1));
+        return ((int)fminf(ceilf(c), 2.1e9f) + (1 << tt_shift) - 1) >> tt_shift << tt_shift;   // whole tiles
+    };
+    auto chunks = [&](int b0, int len) {
+        return b0 + lane < n ? max(1, (int)(((uint32_t)context(b0) + (uint32_t)len - 1) / (uint32_t)len)) : 0;
+    };
+    const int len = max(length(wave), 1 << tt_shift);
+    int count = 0;
+    for (int b0 = 0; b0 < n; b0 += 64) count += gvr_dev::wave_sum(chunks(b0, len));
+    if (lane == 0) lds[wave] = count;
+    __syncthreads();
+    int k = 0;
+    while (k < gvr_kv4::kWaves - 1 && lds[k] > p.units) ++k;
+    Unit r = {-1, 0, 0, 0, max(length(k), 1 << tt_shift)};
+    int before = 0;
+    for (int b0 = 0; b0 < n; b0 += 64) {
+        const int own = chunks(b0, r.chunk), upto = before + gvr_dev::wave_incl_scan(own, lane);
+        const uint64_t past = __ballot(upto > u && b0 + lane < n);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            r.b = b0 + at;
+            r.count = __builtin_amdgcn_readlane(own, at);
+            r.first = __builtin_amdgcn_readlane(upto, at) - r.count;
+            r.split = u - r.first;
+            break;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    r.chunk = __builtin_amdgcn_readfirstlane(r.chunk);
+    return r;
 }
 
 // The work of a workgroup: unit u of U (a sequence's split) and one of `inner`
@@ -309,17 +367,35 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
     const int tg = wave >> p.hw_shift;                    // part of the tile's tokens
     const int tt_shift = 5 + p.tw_shift, TT = 1 << tt_shift;   // tokens of a tile
     const int groups = p.kv_heads >> p.hw_shift;
-    const int64_t units = (int64_t)p.sequences * p.splits;
-    const Job job = job_of(blockIdx.x, units, groups * p.tiles);
-    if (job.unit >= units) return;
+    const Job job = job_of(blockIdx.x, p.units, groups * p.tiles);
+    if (job.unit >= p.units) return;
     const int h = (job.inner % groups << p.hw_shift) + hl, tile = job.inner / groups;
-    const int b = (int)(job.unit / p.splits), split = (int)(job.unit % p.splits);
+    Unit unit = {(int)(job.unit / p.splits), (int)(job.unit % p.splits), p.splits, 0, p.chunk};
+    if (p.balanced) {
+        unit = find_unit(p, (int)job.unit, tt_shift, reinterpret_cast<int32_t*>(lds));
+        if (unit.b < 0) return;
+        if (job.inner == 0 && unit.split == 0 && threadIdx.x == 0) p.units_of[unit.b] = int2{unit.first, unit.count};
+        __syncthreads();   // (the counts' place in LDS)
+    }
+    const int b = unit.b;
 
     const Rows rows = rows_of(p, b);
     const int64_t q0 = rows.q0, nq = rows.nq;
     const int shown = rows.shown;
     if (shown <= 0) return;
     const int64_t held = p.table_width << p.page_shift;
+    const int32_t* table = p.block_table + (int64_t)b * p.table_width;
+    const int64_t lo = (int64_t)unit.split * unit.chunk;
+    // The first tokens' list entries and page numbers are loaded while the
+    // context's length is.
+    int early_tok = -1, early_page = -1;
+    if (p.selection) {
+        const int token = tile / ((p.group + MT * kRows - 1) / (MT * kRows));
+        if (token < shown && lo + threadIdx.x < p.K) early_tok = p.selection[(q0 + token) * p.K + lo + threadIdx.x];
+    } else if (lo + threadIdx.x < held) {
+        early_tok = (int)(lo + threadIdx.x);
+    }
+    if (early_tok >= 0 && early_tok < held) early_page = table[early_tok >> p.page_shift];
     const int ctx = p.pages > 0 ? (int)min((int64_t)max(p.ctx_len[b], 0), held) : 0;
 
     // this lane's query rows; tokens [0, end) of the context or selection concern the tile
@@ -359,12 +435,10 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
     const int all_last =
         list ? 0x7FFFFFFF
              : (int)max((int64_t)-1, p.causal ? ctx - nq + (tile * (MT * kRows)) / p.group : (int64_t)ctx - 1);
-    const int64_t lo = (int64_t)split * p.chunk;
-    const int begin = (int)min(lo, (int64_t)end), stop = (int)min(lo + p.chunk, (int64_t)end);
+    const int begin = (int)min(lo, (int64_t)end), stop = (int)min(lo + unit.chunk, (int64_t)end);
 
     const float scale2 = fabsf(p.scale2);
     const uint32_t record = (uint32_t)p.record;
-    const int32_t* table = p.block_table + (int64_t)b * p.table_width;
     const int page_mask = (1 << p.page_shift) - 1;
 
     // The lane loads 16-byte chunk `quarter` of K and V of token `col` of each
@@ -575,15 +649,16 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
     // steps ahead. The waves of a workgroup read different parts of the same
     // records, so they are kept together: a line that one of them brought into
     // the caches is used by the others before it leaves.
-    for (int piece = begin; piece < stop; piece += kSlots) {
-        const int fill = min(stop - piece, kSlots), padded = (fill + TT - 1) & -TT;
+    for (int piece = begin; piece < stop; piece += L::kSlots) {
+        const int fill = min(stop - piece, L::kSlots), padded = (fill + TT - 1) & -TT;
         lds_barrier();   // the waves are through with the last piece
         for (int i = threadIdx.x; i < padded; i += kThreads) {
             int slot = -1;
             if (i < fill) {
-                const int tok = list ? list[piece + i] : piece + i;
+                const bool early = piece == begin && i < kThreads;
+                const int tok = early ? early_tok : list ? list[piece + i] : piece + i;
                 if (tok >= 0 && (!list || tok <= sel_last)) {
-                    const int page = table[tok >> p.page_shift];
+                    const int page = early ? early_page : table[tok >> p.page_shift];
                     if ((uint32_t)page < (uint32_t)p.pages) slot = (page << p.page_shift) + (tok & page_mask);
                 }
             }
@@ -667,8 +742,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
         // lane: row col, dimensions (4 quarter + i) * NT + n
         const int64_t at = (q0 + qi[mt]) * p.q_heads + h * p.group + qg[mt];
         const float m2 = m[mt] == -INFINITY ? m[mt] : m[mt] * scale2;
-        if (p.splits > 1) {
-            const int64_t part = at * p.splits + split;
+        if (unit.count > 1) {
+            const int64_t part = (job.unit * p.max_q + qi[mt]) * p.q_heads + h * p.group + qg[mt];
             if (quarter == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * part) = float2{m2, sum[mt]};
             if (sum[mt] == 0.f) continue;
             float* po = p.part_o + part * D;
@@ -707,6 +782,7 @@ struct Many {
     static constexpr int kV = kTile * D * 2;               // V
     static constexpr int kS = kTile * D / 32;              // scale bytes of K, then of V
     static constexpr int kBytes = kK + kV + 2 * kS;
+    static constexpr int kSlots = 4096;                    // tokens whose slots the workgroup holds
     static constexpr int kLds = 2 * kBytes + kSlots * 4 + 16;
     static constexpr int kKLoads = kTile * D / 32;         // 16-byte chunks of K
     static constexpr int kVLoads = kTile / 4 * (D / 8);    // 4 tokens x 8 dimensions of V
@@ -784,7 +860,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
     const int32_t* table = p.block_table + (int64_t)b * p.table_width;
     const int page_mask = (1 << p.page_shift) - 1;
     int32_t* const slots = reinterpret_cast<int32_t*>(lds + 2 * M::kBytes);
-    uint32_t* const nan_flag = reinterpret_cast<uint32_t*>(lds + 2 * M::kBytes + kSlots * 4);   // some value is NaN
+    uint32_t* const nan_flag = reinterpret_cast<uint32_t*>(lds + 2 * M::kBytes + M::kSlots * 4);   // some value is NaN
 
     // What this thread moves of a tile.
     v4u kreg[M::kKPer];
@@ -1012,8 +1088,8 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
     };
 
     if (threadIdx.x == 0) *nan_flag = 0u;
-    for (int piece = begin; piece < stop; piece += kSlots) {
-        const int fill = min(stop - piece, kSlots), padded = (fill + M::kTile - 1) / M::kTile * M::kTile;
+    for (int piece = begin; piece < stop; piece += M::kSlots) {
+        const int fill = min(stop - piece, M::kSlots), padded = (fill + M::kTile - 1) / M::kTile * M::kTile;
         lds_barrier();
         for (int i = threadIdx.x; i < padded; i += M::kThreads) {
             int slot = -1;
@@ -1056,7 +1132,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
     const float m2 = m == -INFINITY ? m : m * scale2;
     // lane: row col, dimensions 32 n + 8 b + 4 half + (0 .. 3)
     if (p.splits > 1) {
-        const int64_t part = at * p.splits + split;
+        const int64_t part = (((int64_t)b * p.splits + split) * p.max_q + qi) * p.q_heads + hq;
         if (half == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * part) = float2{m2, sum};
         if (sum == 0.f) return;
         float* po = p.part_o + part * D + 4 * half;
@@ -1092,10 +1168,14 @@ __global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
     const Rows r = rows_of(p, b);
     if (i >= r.shown) return;
     const int64_t at = (r.q0 + i) * p.q_heads + hq;
-    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + at * p.splits;
+    const int2 units = p.balanced ? p.units_of[b] : int2{b * p.splits, p.splits};
+    const int splits = units.y;
+    if (splits == 1) return;               // the unit wrote the result
+    const int64_t step = (int64_t)p.max_q * p.q_heads, first_part = (units.x * (int64_t)p.max_q + i) * p.q_heads + hq;
+    const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + first_part;
     float m = -INFINITY;
-    for (int s = threadIdx.x; s < p.splits; s += 256) {
-        const float2 v = ml[s];
+    for (int s = threadIdx.x; s < splits; s += 256) {
+        const float2 v = ml[s * step];
         m = fmaxf(m, v.y == 0.f ? -INFINITY : v.x);
     }
     for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
@@ -1104,8 +1184,8 @@ __global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
     m = fmaxf(fmaxf(red_l[0], red_l[1]), fmaxf(red_l[2], red_l[3]));
     const float base = m == -INFINITY ? 0.f : m;
     float sum = 0.f;
-    for (int s = threadIdx.x; s < p.splits; s += 256) {
-        const float2 v = ml[s];
+    for (int s = threadIdx.x; s < splits; s += 256) {
+        const float2 v = ml[s * step];
         const float w = v.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(v.x - base);   // 0: it saw nothing and wrote no part
         weight_l[s] = w;
         sum += w * v.y;
@@ -1115,12 +1195,12 @@ __global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
     __syncthreads();
     sum = (red_l[4] + red_l[5]) + (red_l[6] + red_l[7]);
     const int lane = threadIdx.x % kPer, first = threadIdx.x / kPer;
-    const float4* po = reinterpret_cast<const float4*>(p.part_o + at * p.splits * D) + lane;
+    const float4* po = reinterpret_cast<const float4*>(p.part_o + first_part * D) + lane;
     float4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int s = first; s < p.splits; s += kAt) {
+    for (int s = first; s < splits; s += kAt) {
         const float w = weight_l[s];
-        const float4 x = po[(int64_t)s * kPer];
+        const float4 x = po[s * step * kPer];
         const bool seen = w != 0.f;        // (what was not written may be anything)
         acc.x += seen ? w * x.x : 0.f, acc.y += seen ? w * x.y : 0.f;
         acc.z += seen ? w * x.z : 0.f, acc.w += seen ? w * x.w : 0.f;
@@ -1160,7 +1240,7 @@ gvr_status launch(const AttnParams& p, void* stream) {
             go(few_rows_kernel<E, D, 1>);
     }
     if (hipGetLastError() != hipSuccess) return GVR_ERR_HIP;
-    if (p.splits > 1) {
+    if (p.splits > 1 || p.balanced) {
         hipLaunchKernelGGL((combine_kernel<E, D>), dim3((unsigned)((int64_t)p.sequences * p.max_q * p.q_heads)), dim3(256),
                            0, (hipStream_t)stream, p);
         if (hipGetLastError() != hipSuccess) return GVR_ERR_HIP;
@@ -1218,8 +1298,10 @@ gvr_status gvr_kv4_attention(const gvr_kv4_cache* cache, const gvr_kv4_attention
     p.hw_shift = plan.hw_shift, p.tw_shift = plan.tw_shift;
     p.K = a.K, p.causal = a.causal;
     p.scale2 = a.scale * kLog2e;
+    p.balanced = plan.balanced, p.units = plan.units;
     p.part_o = static_cast<float*>(workspace);
-    p.part_ml = p.part_o + (int64_t)a.T * a.q_heads * p.splits * cache->head_dim;
+    p.part_ml = p.part_o + (int64_t)plan.units * plan.max_q * a.q_heads * cache->head_dim;
+    p.units_of = reinterpret_cast<int2*>(p.part_ml + (int64_t)plan.units * plan.max_q * a.q_heads * 2);
     return a.dtype == GVR_BF16 ? launch_d<__bf16>(p, cache->head_dim, stream)
                                : launch_d<_Float16>(p, cache->head_dim, stream);
 }

@@ -53,12 +53,15 @@ constexpr int kRows = 16;          // query rows of a wave
 constexpr int kStep = 32;          // tokens of a wave's step
 constexpr int kWaves = 8;          // of a workgroup
 constexpr int kThreads = 64 * kWaves;
-constexpr int kSlots = 4096;       // tokens whose slots a workgroup holds in LDS
 constexpr int kMaxSplits = 1024;
+constexpr int kMaxBalanced = 2048;  // sequences whose lengths a workgroup adds up
+// The model of plan_attention, in tiles' times.
+constexpr double kPrologue = 3.0;  // of a workgroup: addresses, queries, the first loads
+constexpr double kSecond = 3.0;    // the kernel that joins the splits (and kPart parts read in one)
+constexpr double kPart = 4000.0;
+constexpr double kApart = 0.1;     // share that a tile takes longer for each halving of the heads read together
 constexpr int kCus = 256;          // compute units, each with one workgroup at a time (D = 64: two)
-constexpr int kMinTiles = 4;       // fewest tiles of a workgroup worth another split
 constexpr int kFewRows = 64;       // query rows of a KV head up to which the few-rows kernel serves
-constexpr int kShort = 64;         // steps of a context that one workgroup takes, so that no second kernel runs
 
 // Whether units of workgroups that read the same records are dealt to the eight
 // XCDs: evenly, or so many that it comes to little.
@@ -75,11 +78,15 @@ struct AttnPlan {
     int64_t jobs;     // workgroups
     int splits;       // of a context or selection
     int chunk;        // tokens of a split
+    bool balanced;    // few rows: the kernel sizes the splits by the contexts' lengths, `units` in all
+    int units;        // splits of all sequences
     size_t ws_bytes;
 };
 
-inline size_t partial_bytes(int64_t T, int q_heads, int head_dim, int64_t splits) {
-    return splits > 1 ? (size_t)T * q_heads * splits * (head_dim + 2) * 4 : 0;
+// Workspace for `units` splits of `sequences` sequences (no more units than
+// sequences: none).
+inline size_t partial_bytes(const gvr_kv4_attention_args& a, int max_q, int head_dim, int64_t units) {
+    return units > a.sequences ? (size_t)units * max_q * a.q_heads * (head_dim + 2) * 4 + (size_t)a.sequences * 8 : 0;
 }
 
 inline AttnPlan plan_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_args& a, size_t ws_bytes) {
@@ -107,37 +114,56 @@ inline AttnPlan plan_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_a
         const int64_t most = (n + 4 * unit - 1) / (4 * unit);   // four tiles at least
         splits = splits > most ? most : splits;
         if (splits < 1) splits = 1;
-        while (splits > 1 && partial_bytes(a.T, a.q_heads, c.head_dim, splits) > ws_bytes) --splits;
+        while (splits > 1 && partial_bytes(a, p.max_q, c.head_dim, a.sequences * splits) > ws_bytes) --splits;
         int64_t chunk = ((n + splits - 1) / splits + unit - 1) / unit * unit;
         if (chunk < unit) chunk = unit;
         splits = n > 0 ? (n + chunk - 1) / chunk : 1;
         p.chunk = (int)(chunk > kMaxCount ? kMaxCount / unit * unit : chunk);
         p.splits = (int)splits;
         p.jobs = grid_of((int64_t)a.sequences * c.kv_heads * splits, tiles);
-        p.ws_bytes = partial_bytes(a.T, a.q_heads, c.head_dim, splits);
+        p.balanced = false;
+        p.units = (int)(a.sequences * splits);
+        p.ws_bytes = partial_bytes(a, p.max_q, c.head_dim, p.units);
         return p;
     }
-    // KV heads of a workgroup: all that divide evenly (a record's parts are then
-    // read together), fewer, with more waves to each, while that spares splits
-    // and the contexts still last for several tiles.
+    // Heads of a workgroup (all that divide evenly, or fewer with more waves to
+    // each) and splits, by a model of the time in tiles: a compute unit takes
+    // its workgroups in turn, each for its tiles and for about kPrologue tiles
+    // more (addresses, queries, the first loads); splits cost a second kernel,
+    // and heads apart cost reads of partly used lines.
     const int all = log2_of(kWaves);
-    p.hw_shift = 0;
-    while (p.hw_shift < all && c.kv_heads % (2 << p.hw_shift) == 0) ++p.hw_shift;
-    auto jobs = [&](int hw) { return units * (c.kv_heads >> hw); };
-    auto tiles_of = [&](int hw) { return (steps + (kWaves >> hw) - 1) / (kWaves >> hw); };
-    while (p.hw_shift > 0 && jobs(p.hw_shift) < kCus && tiles_of(p.hw_shift - 1) >= kMinTiles &&
-           (jobs(p.hw_shift - 1) >= kCus / 2 || steps <= kShort))
-        --p.hw_shift;
-    p.tw_shift = all - p.hw_shift;
-    const int64_t fill = c.head_dim == 64 ? 2 * kCus : kCus;
+    int most_hw = 0;
+    while (most_hw < all && c.kv_heads % (2 << most_hw) == 0) ++most_hw;
+    const int64_t resident = kCus * (c.head_dim == 64 && p.row_tiles == 1 && a.dtype == GVR_BF16 ? 2 : 1);
+    double best = -1;
     int64_t splits = 1;
-    if (jobs(p.hw_shift) < kCus && steps > kShort) {
-        splits = jobs(p.hw_shift) > 0 ? (fill + jobs(p.hw_shift) - 1) / jobs(p.hw_shift) : 1;
-        const int64_t most = (tiles_of(p.hw_shift) + kMinTiles - 1) / kMinTiles;
-        splits = splits > most ? most : splits;
+    p.hw_shift = most_hw;
+    auto cost = [&](int hw, int64_t s) {
+        const int64_t wgs = (int64_t)a.sequences * tiles * (c.kv_heads >> hw) * s;
+        const int64_t own = (steps + (kWaves >> hw) * s - 1) / ((kWaves >> hw) * s);
+        const double rounds = (double)((wgs + resident - 1) / resident);
+        const double parts = (double)a.T * a.q_heads * s;
+        return rounds * ((double)own * (1.0 + kApart * (most_hw - hw)) + kPrologue) +
+               (s > 1 ? kSecond + 0.01 * s + parts / kPart : 0.0);
+    };
+    // splits that the workspace holds
+    const size_t each = (size_t)a.sequences * p.max_q * a.q_heads * (c.head_dim + 2) * 4, table = (size_t)a.sequences * 8;
+    const size_t held = ws_bytes > table && each > 0 ? (ws_bytes - table) / each : 0;
+    const int64_t room = held > (size_t)kMaxSplits ? kMaxSplits : (int64_t)held;
+    for (int hw = most_hw; hw >= 0; --hw) {
+        const int64_t wgs = (int64_t)a.sequences * tiles * (c.kv_heads >> hw);
+        const int64_t most = (steps + (kWaves >> hw) - 1) / (kWaves >> hw);
+        for (int k = 0; k <= 6; ++k) {   // unsplit, and what fills a quarter of the device to four rounds
+            int64_t s = k && wgs > 0 ? resident * (1 << k) / (8 * wgs) : 1;
+            s = s > most ? most : s;
+            s = s > kMaxSplits ? kMaxSplits : s;
+            s = s > room ? room : s;
+            if (s < 1) s = 1;
+            const double t = cost(hw, s);
+            if (best < 0 || t < best) best = t, splits = s, p.hw_shift = hw;
+        }
     }
-    if (splits > kMaxSplits) splits = kMaxSplits;
-    while (splits > 1 && partial_bytes(a.T, a.q_heads, c.head_dim, splits) > ws_bytes) --splits;
+    p.tw_shift = all - p.hw_shift;
     const int64_t unit = (int64_t)kStep << p.tw_shift;
     int64_t chunk = (n + splits - 1) / splits;
     chunk = (chunk + unit - 1) / unit * unit;
@@ -145,8 +171,18 @@ inline AttnPlan plan_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_a
     splits = n > 0 ? (n + chunk - 1) / chunk : 1;
     p.chunk = (int)(chunk > kMaxCount ? kMaxCount / unit * unit : chunk);
     p.splits = (int)splits;
-    p.jobs = grid_of((int64_t)a.sequences * splits, tiles * (c.kv_heads >> p.hw_shift));
-    p.ws_bytes = partial_bytes(a.T, a.q_heads, c.head_dim, splits);
+    // Contexts of several sequences are rarely of one length: the kernel cuts
+    // them so that all the units are about as long.
+    p.balanced = splits > 1 && a.sequences > 1 && !a.selection && a.sequences <= kMaxBalanced;
+    p.units = (int)(a.sequences * splits);
+    const int64_t inner = tiles * (c.kv_heads >> p.hw_shift);
+    if (p.balanced) {
+        // (what a round of workgroups leaves over is units too)
+        const int64_t whole = (p.units * inner + resident - 1) / resident * resident / inner;
+        if (whole > p.units && partial_bytes(a, p.max_q, c.head_dim, whole) <= ws_bytes) p.units = (int)whole;
+    }
+    p.jobs = grid_of(p.units, inner);
+    p.ws_bytes = partial_bytes(a, p.max_q, c.head_dim, p.units);
     return p;
 }
 
