@@ -477,3 +477,42 @@ def test_refusals(G):
                dict(k=torch.zeros((3, 2, 64), device=DEV)), dict(v=k.bfloat16()[:2])):
         with pytest.raises(ValueError):
             G.gvr_kv4_read(**{**dict(cache=cache, slots=s, kv_heads=2, head_dim=64), **kw})
+
+
+@pytest.mark.parametrize("shape", [dict(ctx=[700, 60, 0, 3000], nq=1, heads=2, group=4, D=128),
+                                   dict(ctx=[900, 901, 40], nq=3, heads=2, group=8, D=64, dtype="f16"),
+                                   dict(ctx=[640], nq=200, heads=2, group=2, D=128),
+                                   dict(ctx=[300, 513], nq=130, heads=1, group=4, D=64),
+                                   dict(ctx=[500], nq=70, heads=1, group=4, D=256),
+                                   dict(ctx=[2500, 90], nq=2, heads=4, group=24, D=128, K=150)])
+def test_the_same_call_gives_the_same_bits(G, shape):
+    """Eight calls of each kernel, with other work between them, agree bit for bit."""
+    rng = np.random.default_rng(31)
+    ctx, nq, heads, D = shape["ctx"], shape["nq"], shape["heads"], shape["D"]
+    seqs = Sequences(rng, ctx, 16, heads, D)
+    cache, table, lens = seqs.on_gpu()
+    q = torch.randn((len(ctx) * nq, heads * shape["group"], D), device=DEV).to(TORCH[shape.get("dtype", "bf16")])
+    sel = None
+    if shape.get("K"):
+        sel = torch.randint(-1, min(c for c in ctx), (len(ctx) * nq, shape["K"]), device=DEV, dtype=torch.int32)
+    note("same bits: %s" % shape)
+    lse = torch.empty((q.shape[0], q.shape[1]), device=DEV)
+    want = G.gvr_kv4_attention(q, cache, table, lens, heads, selection=sel, lse=lse).clone()
+    first = lse.clone()
+    for i in range(8):
+        torch.randn((1 << (14 + i % 5),), device=DEV)
+        got = G.gvr_kv4_attention(q, cache, table, lens, heads, selection=sel, lse=lse)
+        assert torch.equal(got, want) and torch.equal(lse, first)
+
+
+@pytest.mark.parametrize("n", [2, 63, 64, 65, 130, 700])
+def test_many_sequences_of_uneven_lengths(G, n):
+    """Splits that the kernel sizes: one long context among short and empty ones,
+    more sequences than lanes of a wave, and lengths that are all alike."""
+    rng = np.random.default_rng(n)
+    lengths = [2000] + [int(x) for x in rng.integers(0, 60, n - 1)]
+    rng.shuffle(lengths)
+    attention_case(G, rng, lengths, 1, heads=1, group=2, D=64, page=16)
+    if n <= 130:
+        attention_case(G, rng, [300] * n, 1, heads=2, group=4, D=64, page=64)
+        attention_case(G, rng, lengths, 3, heads=2, group=8, D=64, page=16, dtype="f16", ws=0.7)
