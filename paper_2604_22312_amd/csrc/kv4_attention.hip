@@ -58,7 +58,6 @@ typedef int v8i __attribute__((ext_vector_type(8)));
 template <class E> struct Vec { typedef E x8 __attribute__((ext_vector_type(8))); typedef E x2 __attribute__((ext_vector_type(2))); };
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kBufWord3 = 0x00020000;    // raw buffer resource: 32-bit data format, no swizzle
 constexpr float kLn2 = 0.693147180559945309417f;
 
 struct AttnParams {
@@ -76,7 +75,7 @@ struct AttnParams {
     const int32_t* q_start;
     const int32_t* selection;
     int64_t qt, qh;   // query strides
-    int64_t table_width, record, T, jobs;
+    int64_t table_width, record, T;
     int32_t page_shift, kv_heads, q_heads, group, sequences, uniform_q, max_q, tiles, splits, chunk, K, causal;
     int32_t pages;
     int32_t balanced, units;      // splits sized in the kernel so that the contexts' lengths fill `units`
@@ -291,6 +290,10 @@ DEV int v_place(int tok, int chunk) {
     return ((tok & ~15) + 4 * i + ((tok >> 2) & 3)) * (D / 2) + (chunk ^ (D == 64 ? i & 1 : i)) * 16;
 }
 
+// First token of a step (steps past the last token, of a tile's padding, may
+// start beyond what an int holds: they see none of theirs).
+DEV int step_at(int piece, int t) { return (int)min((uint32_t)piece + (uint32_t)t, 0x7FFFFFE0u); }
+
 DEV void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
@@ -315,24 +318,32 @@ DEV Unit find_unit(const AttnParams& p, int u, int tt_shift, int32_t* lds) {
     const int mine = lane < n ? context_of(p, lane) : 0;
     auto context = [&](int b0) { return b0 == 0 ? mine : b0 + lane < n ? context_of(p, b0 + lane) : 0; };
     float total = 0.f;
-    for (int b0 = 0; b0 < n; b0 += 64) total += gvr_dev::wave_sum_f((float)context(b0));
+    int longest = 0;
+    for (int b0 = 0; b0 < n; b0 += 64) {
+        const int c = context(b0);
+        total += gvr_dev::wave_sum_f((float)c);
+        longest = max(longest, c);
+    }
+    longest = (int)gvr_dev::wave_max_u((uint32_t)longest);
+    // (no context has more than kMaxSplits chunks: what the joining kernel holds)
+    const int floor = max((int)(((uint32_t)longest + kMaxSplits - 1) / kMaxSplits), 1);
     const float least = total / (float)p.units * 0.999999f;
     const float most = total * 1.00001f / (float)(p.units - n) + 1.f;   // (float32 sums: a margin)
     auto length = [&](int k) {
         const float c = least + (most - least) * (float)k * (1.f / (gvr_kv4::kWaves - 1));
-        return ((int)fminf(ceilf(c), 2.1e9f) + (1 << tt_shift) - 1) >> tt_shift << tt_shift;   // whole tiles
+        return (max((int)fminf(ceilf(c), 2.1e9f), floor) + (1 << tt_shift) - 1) >> tt_shift << tt_shift;   // whole tiles
     };
     auto chunks = [&](int b0, int len) {
         return b0 + lane < n ? max(1, (int)(((uint32_t)context(b0) + (uint32_t)len - 1) / (uint32_t)len)) : 0;
     };
-    const int len = max(length(wave), 1 << tt_shift);
+    const int len = length(wave);
     int count = 0;
     for (int b0 = 0; b0 < n; b0 += 64) count += gvr_dev::wave_sum(chunks(b0, len));
     if (lane == 0) lds[wave] = count;
     __syncthreads();
     int k = 0;
     while (k < gvr_kv4::kWaves - 1 && lds[k] > p.units) ++k;
-    Unit r = {-1, 0, 0, 0, max(length(k), 1 << tt_shift)};
+    Unit r = {-1, 0, 0, 0, length(k)};
     int before = 0;
     for (int b0 = 0; b0 < n; b0 += 64) {
         const int own = chunks(b0, r.chunk), upto = before + gvr_dev::wave_incl_scan(own, lane);
@@ -654,11 +665,13 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");   // the next step writes where this one read
     };
 
-    // Pieces of the chunk: slots into LDS, then step after step, the loads two
-    // steps ahead. The waves of a workgroup read different parts of the same
+    // Pieces of the chunk: slots into LDS, then step after step, the loads one
+    // step ahead (two ahead measured no faster: 32 x 32K tokens wait for the
+    // memory either way). The waves of a workgroup read different parts of the same
     // records, so they are kept together: a line that one of them brought into
     // the caches is used by the others before it leaves.
-    for (int piece = begin; piece < stop; piece += L::kSlots) {
+    for (int64_t from = begin; from < stop; from += L::kSlots) {
+        const int piece = (int)from;
         const int fill = min(stop - piece, L::kSlots), padded = (fill + TT - 1) & -TT;
         lds_barrier();   // the waves are through with the last piece
         for (int i = threadIdx.x; i < padded; i += kThreads) {
@@ -697,7 +710,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
             lds_barrier();
         }
         for (int t = first; t < padded; t += TT) {
-            use(d, piece + t, min(t + TT, final));
+            use(d, step_at(piece, t), min(t + TT, final));
             __builtin_amdgcn_s_barrier();
         }
     }
@@ -1095,7 +1108,8 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
     };
 
     if (threadIdx.x == 0) *nan_flag = 0u;
-    for (int piece = begin; piece < stop; piece += M::kSlots) {
+    for (int64_t from = begin; from < stop; from += M::kSlots) {
+        const int piece = (int)from;
         const int fill = min(stop - piece, M::kSlots), padded = (fill + M::kTile - 1) / M::kTile * M::kTile;
         lds_barrier();
         for (int i = threadIdx.x; i < padded; i += M::kThreads) {
@@ -1118,7 +1132,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
             fetch(min(t + 2 * M::kTile, padded - M::kTile));
 #pragma unroll 1
             for (int s = 0; s < M::kTile; s += 32) {
-                const int t0 = piece + t + s;
+                const int t0 = step_at(piece, t + s);
                 if (t0 > wave_last) break;
                 const uint32_t there = (uint32_t)__ballot(slots[t + s + col] >= 0);
                 use(buf, s, t0, there);
@@ -1228,10 +1242,10 @@ __global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
 }
 
 template <class E, int D>
-gvr_status launch(const AttnParams& p, void* stream) {
+gvr_status launch(const AttnParams& p, int64_t jobs, void* stream) {
     if (p.many) {
         typedef Many<D, D == 256 ? 4 : 8> M;
-        hipLaunchKernelGGL((many_rows_kernel<E, D, D == 256 ? 4 : 8>), dim3((unsigned)p.jobs), dim3(M::kThreads), M::kLds,
+        hipLaunchKernelGGL((many_rows_kernel<E, D, D == 256 ? 4 : 8>), dim3((unsigned)jobs), dim3(M::kThreads), M::kLds,
                            (hipStream_t)stream, p);
     } else {
         const int rows = p.row_tiles;
@@ -1239,7 +1253,7 @@ gvr_status launch(const AttnParams& p, void* stream) {
         const int queries = (rows * Query<E, D>::kRuns * Query<E, D>::kPer * 2048) << p.hw_shift;
         const int lds = max(join, WaveLds<D>::kLds + queries);
         auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)p.jobs), dim3(kThreads), lds, (hipStream_t)stream, p);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)jobs), dim3(kThreads), lds, (hipStream_t)stream, p);
         };
         if constexpr (D != 256)
             rows == 2 ? go(few_rows_kernel<E, D, 2>) : go(few_rows_kernel<E, D, 1>);
@@ -1255,8 +1269,8 @@ gvr_status launch(const AttnParams& p, void* stream) {
     return GVR_OK;
 }
 template <class E>
-gvr_status launch_d(const AttnParams& p, int D, void* stream) {
-    return D == 64 ? launch<E, 64>(p, stream) : D == 128 ? launch<E, 128>(p, stream) : launch<E, 256>(p, stream);
+gvr_status launch_d(const AttnParams& p, int64_t jobs, int D, void* stream) {
+    return D == 64 ? launch<E, 64>(p, jobs, stream) : D == 128 ? launch<E, 128>(p, jobs, stream) : launch<E, 256>(p, jobs, stream);
 }
 
 }  // namespace
@@ -1300,7 +1314,7 @@ gvr_status gvr_kv4_attention(const gvr_kv4_cache* cache, const gvr_kv4_attention
     p.kv_heads = cache->kv_heads, p.q_heads = a.q_heads, p.group = a.q_heads / cache->kv_heads;
     p.sequences = a.sequences;
     p.uniform_q = a.q_start ? 0 : (int32_t)(a.T / a.sequences);
-    p.max_q = plan.max_q, p.tiles = plan.tiles, p.jobs = plan.jobs, p.splits = plan.splits, p.chunk = plan.chunk;
+    p.max_q = plan.max_q, p.tiles = plan.tiles, p.splits = plan.splits, p.chunk = plan.chunk;
     p.many = plan.many, p.row_tiles = plan.row_tiles;
     p.hw_shift = plan.hw_shift, p.tw_shift = plan.tw_shift;
     p.K = a.K, p.causal = a.causal;
@@ -1309,8 +1323,8 @@ gvr_status gvr_kv4_attention(const gvr_kv4_cache* cache, const gvr_kv4_attention
     p.part_o = static_cast<float*>(workspace);
     p.part_ml = p.part_o + (int64_t)plan.units * plan.max_q * a.q_heads * cache->head_dim;
     p.units_of = reinterpret_cast<int2*>(p.part_ml + (int64_t)plan.units * plan.max_q * a.q_heads * 2);
-    return a.dtype == GVR_BF16 ? launch_d<__bf16>(p, cache->head_dim, stream)
-                               : launch_d<_Float16>(p, cache->head_dim, stream);
+    return a.dtype == GVR_BF16 ? launch_d<__bf16>(p, plan.jobs, cache->head_dim, stream)
+                               : launch_d<_Float16>(p, plan.jobs, cache->head_dim, stream);
 }
 
 }  // extern "C"

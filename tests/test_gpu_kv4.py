@@ -516,3 +516,30 @@ def test_many_sequences_of_uneven_lengths(G, n):
     if n <= 130:
         attention_case(G, rng, [300] * n, 1, heads=2, group=4, D=64, page=64)
         attention_case(G, rng, lengths, 3, heads=2, group=8, D=64, page=16, dtype="f16", ws=0.7)
+
+
+def test_one_long_sequence_among_empty_ones(G):
+    """The kernel sizes the splits: all but a few would go to the one long context,
+    more than the kernel that joins them holds, were their number not bounded."""
+    rng = np.random.default_rng(41)
+    attention_case(G, rng, [0] * 40 + [600000] + [0] * 22 + [3, 0], 1, heads=1, group=2, D=64, page=64)
+
+
+@pytest.mark.parametrize("nq", [1, 40])
+def test_longest_context(G, nq):
+    """2^31 - 16 tokens, all but those of three pages invisible: places past the
+    last step must not pass the end of 32 bits."""
+    page, H, D, group = 16, 1, 64, 2
+    width = 2 ** 27 - 1
+    rng = np.random.default_rng(42)
+    cache = random_cache(rng, 3, page, H, D)
+    table = torch.full((1, width), -1, dtype=torch.int32, device=DEV)
+    for i, at in enumerate((5, 70000000, width - 1)):
+        table[0, at] = i
+    lens = torch.tensor([width * page], dtype=torch.int32, device=DEV)
+    q = torch.randn((nq, H * group, D), device=DEV).bfloat16()
+    note("attention over 2^31 - 16 tokens, %d query tokens" % nq)
+    out = G.gvr_kv4_attention(q, torch.from_numpy(cache).to(DEV), table, lens, H, causal=False)
+    s = Sequences.__new__(Sequences)
+    s.table, s.cache, s.ctx, s.page, s.heads, s.D = np.array([[0, 1, 2]]), cache, [3 * page], page, H, D
+    check_attention(out, None, q, s, [0, nq], D ** -0.5, causal=False, what="longest context")
