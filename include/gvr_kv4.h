@@ -67,8 +67,8 @@ gvr_status gvr_kv4_append(const gvr_kv4_cache* cache, const gvr_heads* k, const 
 
 /* Read T tokens back: k and v [T][kv_heads][head_dim] of type `dtype` receive
  * the values that the records at slots [T] stand for (exact in bfloat16 and
- * float32, where only a code of 2^128 overflows; rounded in float16); zeros for a slot outside the cache. Either of
- * k and v may be NULL. Errors as gvr_kv4_append. */
+ * float32, where only a code of 2^128 overflows; rounded in float16); zeros
+ * for a slot outside the cache. Either of k and v may be NULL. Errors as gvr_kv4_append. */
 gvr_status gvr_kv4_read(const gvr_kv4_cache* cache, const gvr_heads* k, const gvr_heads* v, int32_t dtype, int64_t T,
                         const int64_t* slots, void* stream);
 
@@ -89,13 +89,18 @@ gvr_status gvr_kv4_read(const gvr_kv4_cache* cache, const gvr_heads* k, const gv
  * A query that sees no token gives out = 0. Masked tokens are never part of a
  * result, whatever their records hold (NaN blocks included).
  *
- * Numerics: q and the stored values enter the matrix cores as they are (a
- * stored value is exact in the 16-bit type; with float16 queries it must be
- * below 65520), products accumulate in float32, the softmax's maximum and sum
- * are float32, the weights are rounded to the 16-bit type for the second
- * product, and the result is rounded once. Rounding depends on how the
- * context is split (the workspace below), never on timing: the same call
- * gives the same bits. */
+ * Numerics: the stored keys enter the matrix cores as they are, the queries as
+ * sums of two 8-bit numbers (three for float16) with a common scale per 32
+ * elements: exact down to 2^-14 (2^-18) of the block's largest magnitude and
+ * off by at most 2^-21 (2^-25) of it below. A score sums in float32 and is off
+ * by about 2^-16 of scale * sum |q k|. The softmax's maximum and sum are
+ * float32; the weights, at most 1, and the stored values (exact; with float16
+ * queries they must be below 65520) enter the second product in the queries'
+ * type; it sums in float32, and the result is rounded once: about 0.0017
+ * relative error in bfloat16, of which 0.0016 is that last rounding. Rounding
+ * depends on how the context is split (the workspace below, and with several
+ * sequences their lengths), never on timing: the same call gives the same
+ * bits. */
 typedef struct gvr_kv4_attention_args {
     const void* q;               /* [T][q_heads][head_dim], 16-byte aligned rows */
     int64_t q_token_stride;      /* elements, multiples of 8 */

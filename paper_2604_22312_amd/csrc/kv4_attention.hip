@@ -29,9 +29,25 @@
 // of 2048 selected tokens 0.0017 against 0.0019, 0.0016 being the output's own
 // rounding.)
 //
-// A workgroup is `hw` KV heads x `tw` waves that take turns at the steps of
-// one chunk of a context; its waves are joined in LDS, chunks of a context by
-// a second kernel from float32 partial results.
+// A workgroup is `hw` KV heads x `tw` waves (eight in all) that take turns at
+// the steps of one chunk of a context; its waves are joined in LDS, chunks of a
+// context by a second kernel from float32 partial results, in a fixed order. A
+// unit is one chunk of one sequence. Chunks are of one length that the host
+// chooses, or, for several sequences, of one that every workgroup works out
+// from the contexts' lengths (48 contexts of 0 .. 16K tokens: 43 us against
+// 59 with the host's). Units that read the same records go to one XCD.
+//
+// What bounds it, measured (MI355X; a plain read of as many bytes in brackets):
+//   32 x 32K tokens, 8 KV heads of 128, 4 rows each: 209 us = 5.5 TB/s (166 us);
+//     memory: the same loads with nothing computed take 205 us, because a head's
+//     64 bytes of codes per record are half a line, and its eight waves do not
+//     ask for both halves at once;
+//   1 x 512K tokens, 8 rows: 117 us (83 us): the same, and the join of 256 parts;
+//   128 rows of 2048 selected tokens: 64 us (41 us for what the rows select
+//     one by one, 24 for what two draft rows have in common): gathers of 1 KB;
+//   1 x 1K tokens: 12.6 us: latency, of two launches and in the first of them
+//     length -> page -> record -> join.
+// More than 64 rows of a KV head: see "many query rows" below.
 
 #include <hip/hip_runtime.h>
 
@@ -377,7 +393,13 @@ DEV Job job_of(uint32_t bid, int64_t units, int inner) {
     return {bid / (uint32_t)inner, (int)(bid % (uint32_t)inner)};
 }
 
-// MT: row tiles of 16 that a wave serves with one pass over K and V.
+// MT: row tiles of 16 that a wave serves with one pass over K and V. Two where
+// more than 16 rows share their tokens: the bytes are read and V is unpacked
+// once for both (32 x 8K tokens, 8 heads of 128: 32 rows 93 us against 129,
+// 64 rows 160 against 226). D = 256 has no registers for two.
+// Registers: one workgroup to a compute unit (256 a lane), but two where 128
+// suffice without spills, which is D = 64, MT = 1 in bfloat16: 32 x 32K tokens
+// 159 us against 174, small calls within 2 us either way.
 template <class E, int D, int MT>
 __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16) ? 4 : 2) void few_rows_kernel(AttnParams p) {
     constexpr int NT = D / 16;        // dimensions of V per lane = matrix steps of the second product
@@ -795,7 +817,14 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
 // kernel (a lane's column l % 32 is its row, half l / 32). The context goes
 // through LDS in tiles of 16 NW tokens: K as stored, V as 16-bit floats,
 // transposed (a row of tokens per dimension, in the order in which the
-// scores' registers name them), unpacked once for all the rows.
+// scores' registers name them), unpacked once for all the rows. Two buffers: a
+// tile is unpacked into one while the other is used, and the records of the
+// tile after it are on their way in registers.
+// 4096 rows of 32 heads over 32K tokens, 8 KV heads of 128: 1.93 ms, 1.07
+// PFLOP/s, against 3.83 ms with the few-rows kernel. Bound by the vector unit
+// beside the matrix cores: exponentials, packing and the unpacking of V. For 64
+// rows and fewer the few-rows kernel is ahead (32 x 8K tokens: 160 us against
+// 235; 96 rows 266 against 255): half of this one's rows are then empty.
 template <int D, int NW>
 struct Many {
     static constexpr int kThreads = 64 * NW;

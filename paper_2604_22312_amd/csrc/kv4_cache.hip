@@ -7,7 +7,11 @@
 // conversion packs two codes per instruction (round to nearest even,
 // saturating: what the format asks). A thread serves heads_each heads of its
 // token in turn with the same cosines. Bound by HBM: a key and value element
-// is read once and 4.25 bits of each written.
+// is read once and 4.25 bits of each written (16384 tokens of 8 heads of 128
+// with rotation, appended and read back from HBM: 43 us = 4.1 TB/s; the append
+// alone, what it reads still in the caches, 19, the reading 15); one token: 4 us
+// each, the launch. Unaligned rows load element by element (append 19 us
+// against 43).
 
 #include <hip/hip_runtime.h>
 

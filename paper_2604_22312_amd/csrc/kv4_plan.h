@@ -61,10 +61,14 @@ constexpr double kSecond = 3.0;    // the kernel that joins the splits (and kPar
 constexpr double kPart = 4000.0;
 constexpr double kApart = 0.1;     // share that a tile takes longer for each halving of the heads read together
 constexpr int kCus = 256;          // compute units, each with one workgroup at a time (D = 64: two)
-constexpr int kFewRows = 64;       // query rows of a KV head up to which the few-rows kernel serves
+// Query rows of a KV head up to which the few-rows kernel serves (32 contexts of
+// 8K, 8 heads of 128: few / many rows 160 / 235 us at 64 rows, 266 / 255 at 96,
+// 278 / 269 at 128).
+constexpr int kFewRows = 64;
 
 // Whether units of workgroups that read the same records are dealt to the eight
-// XCDs: evenly, or so many that it comes to little.
+// XCDs: evenly, or so many that it comes to little (32 contexts of 8K, 64 rows
+// in two tiles: 160 us, and 169 where neighbours go to different XCDs).
 inline bool by_xcd(int64_t units) { return units % 8 == 0 || units >= 64; }
 inline int64_t grid_of(int64_t units, int64_t inner) { return (by_xcd(units) ? (units + 7) / 8 * 8 : units) * inner; }
 
@@ -130,7 +134,8 @@ inline AttnPlan plan_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_a
     // each) and splits, by a model of the time in tiles: a compute unit takes
     // its workgroups in turn, each for its tiles and for about kPrologue tiles
     // more (addresses, queries, the first loads); splits cost a second kernel,
-    // and heads apart cost reads of partly used lines.
+    // and heads apart cost reads of partly used lines (32 x 32K tokens, 8 heads
+    // of 128: 242 us all together, 276 in twos; 1 x 16K: 16.0 and 15.8).
     const int all = log2_of(kWaves);
     int most_hw = 0;
     while (most_hw < all && c.kv_heads % (2 << most_hw) == 0) ++most_hw;

@@ -6,7 +6,13 @@
 // consecutive ones) or copies sixteen elements behind the rotary ones, for
 // heads_each heads of one token in turn, so that the eight cosines and sines
 // are read once for all of them. Bound by HBM: each element is read once and
-// written once.
+// written once (8192 tokens of 32 heads of 128 in bfloat16, 138 MB with the
+// table: 29.9 us = 4.6 TB/s, where a copy of 1 GB reaches 4.8; 35 MB of float32:
+// 11.3 us); small
+// calls by their launch (4.5 us).
+// Rows that are not 16-byte aligned, or whose rotary part is no multiple of 16,
+// take a kernel that loads element by element (8192 x 64 x 128 in bfloat16:
+// 51 us wide, 55 us by element; 1024 x 32: 5.1 and 6.0).
 
 #include <hip/hip_runtime.h>
 

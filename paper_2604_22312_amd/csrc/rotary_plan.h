@@ -44,7 +44,10 @@ struct Launch {
 };
 inline Launch plan_items(int64_t T, int heads, int per_head, int most_heads_each) {
     Launch p;
-    // enough threads to fill the device come before reuse of the cosines
+    // Enough threads to fill the device come before reuse of the cosines: four
+    // heads each against one, 8192 tokens x 64 heads of 128 51 us against 60, an
+    // append of 16384 x 8 heads 19 us against 27; 1024 x 32 the other way, 6.6
+    // and 5.5 us, and 5.1 us with the two heads each that this rule takes.
     const int64_t fill = (int64_t)256 * 2048, items = T * (int64_t)heads;
     p.heads_each = 1;
     while (p.heads_each < most_heads_each && p.heads_each < heads &&
