@@ -34,20 +34,23 @@
 // context by a second kernel from float32 partial results, in a fixed order. A
 // unit is one chunk of one sequence. Chunks are of one length that the host
 // chooses, or, for several sequences, of one that every workgroup works out
-// from the contexts' lengths (48 contexts of 0 .. 16K tokens: 43 us against
-// 59 with the host's). Units that read the same records go to one XCD.
+// from the contexts' lengths (48 contexts of 0 .. 16K tokens, waves together
+// every step: 43 us against 59 with the host's). Units that read the same records go to one XCD.
 //
 // What bounds it, measured (MI355X; a plain read of as many bytes in brackets):
-//   32 x 32K tokens, 8 KV heads of 128, 4 rows each: 209 us = 5.5 TB/s (166 us);
+//   32 x 32K tokens, 8 KV heads of 128, 4 rows each: 208 us = 5.5 TB/s (166 us);
 //     memory: the same loads with nothing computed take 205 us, because a head's
 //     64 bytes of codes per record are half a line, and its eight waves do not
 //     ask for both halves at once;
-//   1 x 512K tokens, 8 rows: 117 us (83 us): the same, and the join of 256 parts;
-//   128 rows of 2048 selected tokens: 64 us (41 us for what the rows select
+//   1 x 512K tokens, 8 rows: 116 us (83 us): the same, and the join of 256 parts;
+//   128 rows of 2048 selected tokens: 61 us (41 us for what the rows select
 //     one by one, 24 for what two draft rows have in common): gathers of 1 KB;
+//   48 x 3 rows over 0 .. 16K tokens, 2 KV heads of 64, float16: 34 us (7.5 us):
+//     12 us before the first record (lengths, splits, pages), 6 of join, and steps at
+//     2.6 TB/s, which two row tiles of dependent products and exponentials set;
 //   1 x 1K tokens: 12.6 us: latency, of two launches and in the first of them
 //     length -> page -> record -> join.
-// More than 64 rows of a KV head: see "many query rows" below.
+// More than 128 rows of a KV head: see "many query rows" below.
 
 #include <hip/hip_runtime.h>
 
@@ -395,8 +398,9 @@ DEV Job job_of(uint32_t bid, int64_t units, int inner) {
 
 // MT: row tiles of 16 that a wave serves with one pass over K and V. Two where
 // more than 16 rows share their tokens: the bytes are read and V is unpacked
-// once for both (32 x 8K tokens, 8 heads of 128: 32 rows 93 us against 129,
-// 64 rows 160 against 226). D = 256 has no registers for two.
+// once for both (32 x 8K tokens, 8 heads of 128, waves together every step: 32
+// rows 93 us against 129, 64 rows 160 against 226). D = 256 has no registers
+// for two.
 // Registers: one workgroup to a compute unit (256 a lane), but two where 128
 // suffice without spills, which is D = 64, MT = 1 in bfloat16: 32 x 32K tokens
 // 159 us against 174, small calls within 2 us either way.
@@ -691,7 +695,14 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
     // step ahead (two ahead measured no faster: 32 x 32K tokens wait for the
     // memory either way). The waves of a workgroup read different parts of the same
     // records, so they are kept together: a line that one of them brought into
-    // the caches is used by the others before it leaves.
+    // the caches is used by the others before it leaves. How often depends on
+    // what a step computes and reads: where more is computed the memory is less of
+    // a bound, and waves gain from being at different places of a step; selected
+    // records are apart in any case. Every step, every second, every sixteenth
+    // (us): 32 x 32K tokens, D = 64 152, 155, 163, D = 128 (not in the caches) 210,
+    // 212, -; 128 rows of 2048 selected 63.7, 61.4, 63.9; two row tiles, 64 rows
+    // over 32 x 8K 160, 146, 138; D = 256, 16 x 8K 71, 68, 66.
+    const int together = MT == 2 || D == 256 ? 15 : list ? 1 : 0;   // less one
     for (int64_t from = begin; from < stop; from += L::kSlots) {
         const int piece = (int)from;
         const int fill = min(stop - piece, L::kSlots), padded = (fill + TT - 1) & -TT;
@@ -733,7 +744,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
         }
         for (int t = first; t < padded; t += TT) {
             use(d, step_at(piece, t), min(t + TT, final));
-            __builtin_amdgcn_s_barrier();
+            if (((t >> tt_shift) & together) == together) __builtin_amdgcn_s_barrier();
         }
     }
 #pragma unroll
@@ -822,9 +833,10 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
 // tile after it are on their way in registers.
 // 4096 rows of 32 heads over 32K tokens, 8 KV heads of 128: 1.93 ms, 1.07
 // PFLOP/s, against 3.83 ms with the few-rows kernel. Bound by the vector unit
-// beside the matrix cores: exponentials, packing and the unpacking of V. For 64
-// rows and fewer the few-rows kernel is ahead (32 x 8K tokens: 160 us against
-// 235; 96 rows 266 against 255): half of this one's rows are then empty.
+// beside the matrix cores: exponentials, packing and the unpacking of V. For 128
+// rows and fewer the few-rows kernel is ahead (32 x 8K tokens: 64 rows 139 us
+// against 234, 128 rows 256 against 274, 192 rows 398 against 348): half of this
+// one's rows are then empty.
 template <int D, int NW>
 struct Many {
     static constexpr int kThreads = 64 * NW;
@@ -1223,6 +1235,9 @@ __global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
     if (splits == 1) return;               // the unit wrote the result
     const int64_t step = (int64_t)p.max_q * p.q_heads, first_part = (units.x * (int64_t)p.max_q + i) * p.q_heads + hq;
     const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + first_part;
+    const int lane = threadIdx.x % kPer, first = threadIdx.x / kPer;
+    const float4* po = reinterpret_cast<const float4*>(p.part_o + first_part * D) + lane;
+    const float4 x0 = po[min(first, splits - 1) * step * kPer];   // (with the weights' loads)
     float m = -INFINITY;
     for (int s = threadIdx.x; s < splits; s += 256) {
         const float2 v = ml[s * step];
@@ -1244,17 +1259,15 @@ __global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
     if ((threadIdx.x & 63) == 0) red_l[4 + (threadIdx.x >> 6)] = sum;
     __syncthreads();
     sum = (red_l[4] + red_l[5]) + (red_l[6] + red_l[7]);
-    const int lane = threadIdx.x % kPer, first = threadIdx.x / kPer;
-    const float4* po = reinterpret_cast<const float4*>(p.part_o + first_part * D) + lane;
     float4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int s = first; s < splits; s += kAt) {
-        const float w = weight_l[s];
-        const float4 x = po[s * step * kPer];
+    auto add = [&](float w, const float4& x) {
         const bool seen = w != 0.f;        // (what was not written may be anything)
         acc.x += seen ? w * x.x : 0.f, acc.y += seen ? w * x.y : 0.f;
         acc.z += seen ? w * x.z : 0.f, acc.w += seen ? w * x.w : 0.f;
-    }
+    };
+    if (first < splits) add(weight_l[first], x0);
+#pragma unroll 8
+    for (int s = first + kAt; s < splits; s += kAt) add(weight_l[s], po[s * step * kPer]);
     acc_l[threadIdx.x] = acc;
     __syncthreads();
     if (first != 0) return;

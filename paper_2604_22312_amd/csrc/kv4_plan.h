@@ -62,9 +62,10 @@ constexpr double kPart = 4000.0;
 constexpr double kApart = 0.1;     // share that a tile takes longer for each halving of the heads read together
 constexpr int kCus = 256;          // compute units, each with one workgroup at a time (D = 64: two)
 // Query rows of a KV head up to which the few-rows kernel serves (32 contexts of
-// 8K, 8 heads of 128: few / many rows 160 / 235 us at 64 rows, 266 / 255 at 96,
-// 278 / 269 at 128).
-constexpr int kFewRows = 64;
+// 8K, 8 heads of 128: few / many rows 139 / 234 us at 64 rows, 256 / 274 at 128,
+// 398 / 348 at 192; 16 of 8K, 4 heads: D = 64, 128 rows 58 / 71, D = 256 149 / 171;
+// one of 64K: 128 rows 79 / 82, 192 rows 112 / 104).
+constexpr int kFewRows = 128;
 
 // Whether units of workgroups that read the same records are dealt to the eight
 // XCDs: evenly, or so many that it comes to little (32 contexts of 8K, 64 rows

@@ -543,3 +543,23 @@ def test_longest_context(G, nq):
     s = Sequences.__new__(Sequences)
     s.table, s.cache, s.ctx, s.page, s.heads, s.D = np.array([[0, 1, 2]]), cache, [3 * page], page, H, D
     check_attention(out, None, q, s, [0, nq], D ** -0.5, causal=False, what="longest context")
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_rows_around_the_kernels_change(G, D, dtype):
+    """127 to 130 rows of a KV head (few-rows kernel up to 128), NaN records beside the
+    visible ones, ragged query counts, and a workspace that allows some splits only."""
+    rng = np.random.default_rng(51)
+    attention_case(G, rng, [333], 127, heads=2, group=1, D=D, dtype=dtype)
+    attention_case(G, rng, [333], 129, heads=1, group=1, D=D, dtype=dtype)
+    attention_case(G, rng, [500, 70], 26, heads=1, group=5, D=D, dtype=dtype, ws=0.5)
+    attention_case(G, rng, [700, 90, 0, 200], [150, 90, 3, 1], heads=2, group=1, D=D, dtype=dtype, ws=0.6)
+    attention_case(G, rng, [400, 90], [40, 7], heads=1, group=3, D=D, dtype=dtype, causal=False, page=64)
+
+
+def test_one_sequence_many_rows_split(G):
+    """Many rows over a long context: splits of the many-rows kernel, joined."""
+    rng = np.random.default_rng(52)
+    attention_case(G, rng, [9000], 40, heads=1, group=4, D=128, page=64)
+    attention_case(G, rng, [9000], 40, heads=1, group=4, D=128, page=64, dtype="f16", causal=False, ws=0.4)
