@@ -45,20 +45,20 @@ DEV void store8(E* p, f8 v) {
 // aligned row, or one by one.
 template <int NP, bool WIDE>
 DEV void load_cs(const float* row, int i, float (&c)[NP], float (&s)[NP]) {
-    if (!row) {
-#pragma unroll
-        for (int j = 0; j < NP; ++j) c[j] = s[j] = __builtin_nanf("");
-        return;
-    }
+    const float nan = __builtin_nanf("");
     if constexpr (WIDE) {
+        float4 v[NP / 2];
 #pragma unroll
-        for (int j = 0; j < NP; j += 2) {
-            const float4 v = *reinterpret_cast<const float4*>(row + 2 * (i + j));
-            c[j] = v.x, s[j] = v.y, c[j + 1] = v.z, s[j + 1] = v.w;
+        for (int j = 0; j < NP / 2; ++j) v[j] = float4{nan, nan, nan, nan};
+        if (row) {
+#pragma unroll
+            for (int j = 0; j < NP / 2; ++j) v[j] = *reinterpret_cast<const float4*>(row + 2 * (i + 2 * j));
         }
+#pragma unroll
+        for (int j = 0; j < NP; j += 2) c[j] = v[j / 2].x, s[j] = v[j / 2].y, c[j + 1] = v[j / 2].z, s[j + 1] = v[j / 2].w;
     } else {
 #pragma unroll
-        for (int j = 0; j < NP; ++j) c[j] = row[2 * (i + j)], s[j] = row[2 * (i + j) + 1];
+        for (int j = 0; j < NP; ++j) c[j] = row ? row[2 * (i + j)] : nan, s[j] = row ? row[2 * (i + j) + 1] : nan;
     }
 }
 
