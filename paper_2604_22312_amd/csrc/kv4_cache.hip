@@ -8,9 +8,9 @@
 // saturating: what the format asks). A thread serves heads_each heads of its
 // token in turn with the same cosines. Bound by HBM: a key and value element
 // is read once and 4.25 bits of each written (16384 tokens of 8 heads of 128
-// with rotation, appended and read back from HBM: 43 us = 4.1 TB/s; the append
+// with rotation, appended and read back from HBM: 43 us = 4.2 TB/s; the append
 // alone, what it reads still in the caches, 19, the reading 15); one token: 4 us
-// each, the launch. Unaligned rows load element by element (append 19 us
+// each, the launch. Unaligned rows load element by element (append 18 us
 // against 43).
 
 #include <hip/hip_runtime.h>
@@ -221,7 +221,7 @@ gvr_status token_params(const gvr_kv4_cache* cache, const gvr_heads* k, const gv
     p->H = cache->kv_heads, p->D = cache->head_dim;
     p->positions = nullptr, p->cs = nullptr, p->n_pos = 0, p->rot = 0, p->inter = false;
     if (T > 0) {
-        *l = gvr_rot::plan_items(T, p->H, p->D / 8, 4);
+        *l = gvr_rot::plan_items(T, p->H, p->D / 8, 2);
         p->heads_each = l->heads_each;
         p->head_groups = l->head_groups;
         p->tokens = l->tokens;

@@ -7,12 +7,12 @@
 // heads_each heads of one token in turn, so that the eight cosines and sines
 // are read once for all of them. Bound by HBM: each element is read once and
 // written once (8192 tokens of 32 heads of 128 in bfloat16, 138 MB with the
-// table: 29.9 us = 4.6 TB/s, where a copy of 1 GB reaches 4.8; 35 MB of float32:
-// 11.3 us); small
+// table: 27.9 us = 4.95 TB/s, where a copy of 1 GB reaches 4.8; 35 MB of float32:
+// 10.5 us); small
 // calls by their launch (4.5 us).
 // Rows that are not 16-byte aligned, or whose rotary part is no multiple of 16,
 // take a kernel that loads element by element (8192 x 64 x 128 in bfloat16:
-// 51 us wide, 55 us by element; 1024 x 32: 5.1 and 6.0).
+// 42 us wide, 55 us by element; 1024 x 32: 4.8 and 6.2).
 
 #include <hip/hip_runtime.h>
 
@@ -156,7 +156,7 @@ __global__ __launch_bounds__(gvr_yarn::kMaxPairs) void rope_table_kernel(int64_t
 template <class E>
 gvr_status launch_rotate(RotParams p, bool wide, bool inter, void* stream) {
     p.per_head = wide ? p.D / 16 : p.rot / 2 + p.D - p.rot;
-    const gvr_rot::Launch l = gvr_rot::plan_items(p.T, p.H, p.per_head, 8);
+    const gvr_rot::Launch l = gvr_rot::plan_items(p.T, p.H, p.per_head, 2);
     p.heads_each = l.heads_each;
     p.head_groups = l.head_groups;
     p.tokens = l.tokens;

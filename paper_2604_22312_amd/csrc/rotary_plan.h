@@ -44,10 +44,12 @@ struct Launch {
 };
 inline Launch plan_items(int64_t T, int heads, int per_head, int most_heads_each) {
     Launch p;
-    // Enough threads to fill the device come before reuse of the cosines: four
-    // heads each against one, 8192 tokens x 64 heads of 128 51 us against 60, an
-    // append of 16384 x 8 heads 19 us against 27; 1024 x 32 the other way, 6.6
-    // and 5.5 us, and 5.1 us with the two heads each that this rule takes.
+    // Several heads (both callers: two) where that leaves threads enough to fill
+    // the device. One, two,
+    // four each (us): rotation of 8192 tokens x 32 heads of 128 28.0, 27.9, 29.6,
+    // x 64 heads 40.9, 41.6, 43.6; append of 16384 x 8 heads 22.4, 18.7, 17.8, and
+    // read back from HBM 44.1, 42.6, 42.9. Small calls need the threads: 128 x 64
+    // heads 4.2 with one, 5.2 with four; an append of 64 x 8 heads 4.2 and 5.5.
     const int64_t fill = (int64_t)256 * 2048, items = T * (int64_t)heads;
     p.heads_each = 1;
     while (p.heads_each < most_heads_each && p.heads_each < heads &&
