@@ -28,7 +28,7 @@ def _gpu():
 
 
 def held(layer, ctx):
-    """The layer's sequences as the tests' checker takes them."""
+    """The layer's sequences as the tests' comparison takes them."""
     s = Sequences.__new__(Sequences)
     s.table, s.cache = layer.blocks.cpu().numpy(), layer.cache.cpu().numpy()
     s.ctx, s.page, s.heads, s.D = list(ctx), layer.page, layer.kv_heads, layer.D
