@@ -1251,8 +1251,9 @@ __global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
     float sum = 0.f;
     for (int s = threadIdx.x; s < splits; s += 256) {
         const float2 v = ml[s * step];
-        const float w = v.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(v.x - base);   // 0: it saw nothing and wrote no part
-        weight_l[s] = w;
+        const bool wrote = v.y != 0.f;     // (else it saw nothing)
+        const float w = wrote ? __builtin_amdgcn_exp2f(v.x - base) : 0.f;
+        weight_l[s] = wrote ? w : -1.f;
         sum += w * v.y;
     }
     for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
@@ -1261,7 +1262,9 @@ __global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
     sum = (red_l[4] + red_l[5]) + (red_l[6] + red_l[7]);
     float4 acc = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](float w, const float4& x) {
-        const bool seen = w != 0.f;        // (what was not written may be anything)
+        // What was not written may be anything. A part whose weight is zero counts:
+        // a NaN that its row sees stays one, as without splits.
+        const bool seen = !(w < 0.f);
         acc.x += seen ? w * x.x : 0.f, acc.y += seen ? w * x.y : 0.f;
         acc.z += seen ? w * x.z : 0.f, acc.w += seen ? w * x.w : 0.f;
     };
