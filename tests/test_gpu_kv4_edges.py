@@ -60,3 +60,49 @@ def test_visible_nan_of_a_part_without_weight(G, dtype, D, nq):
             # the weights are 0 and 1: sums in float32 and one rounding
             tol = UNIT[dtype] * np.abs(ref) + 2 * (n + 64) * 2.0 ** -24 * mag + 2.0 ** -24
             assert (np.abs(out[i] - ref) <= tol)[:, ~nan].all()
+
+
+def one_ahead(n, D, value, rng):
+    """k, v of n tokens: all scores 0 but those of token 7, whose value is given; the others' values lie in 1 .. 6."""
+    k, v = np.zeros((n, 1, D)), rng.uniform(1.0, 6.0, (n, 1, D))
+    k[7, 0, 0], v[7] = 6.0, value
+    return k, v
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("nq", [1, 70])
+@pytest.mark.parametrize("ahead", [16.0, 17.5, 20.0])
+def test_float16_keeps_the_tail_behind_a_large_score(G, D, nq, ahead):
+    """One token far ahead whose value is zero: the result is the sum of the many small weights, each of which may carry
+    one float16 rounding and 2^-40 of the largest."""
+    rng = np.random.default_rng(62)
+    n = 20001
+    cache, table, lens, kk, vv = held(*one_ahead(n, D, 0.0, rng), page=64)
+    q = torch.zeros((nq, 2, D), dtype=torch.float16, device=DEV)
+    q[:, :, 0] = 1.0
+    u, eps = UNIT["f16"], ((D + 8) * ahead + n + 64) * 2.0 ** -24
+    for ws in (torch.empty(0, dtype=torch.uint8, device=DEV), None):
+        note("float16 tail: D=%d nq=%d ahead=%s %s" % (D, nq, ahead, "split" if ws is None else "whole"))
+        lse = torch.empty((nq, 2), device=DEV)
+        out = f64(G.gvr_kv4_attention(q, cache, table, lens, 1, scale=ahead / 6.0, causal=False, workspace=ws, lse=lse))
+        ref, ref_lse, mag = O.attention(f64(q)[0], kk, vv, ahead / 6.0)
+        tol = (u + 2 * eps) * (1 + u) * mag + u * np.abs(ref) + n * 2.0 ** -40 * 6.0 + 2.0 ** -25
+        assert (tol < 0.01 * ref).all()
+        assert (np.abs(out - ref) <= tol).all(), "off by %.3g of the result" % (np.abs(out - ref) / ref).max()
+        assert (np.abs(f64(lse) - ref_lse) <= 2 * eps + 4 * 2.0 ** -24 * (ref_lse + 1)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("nq", [1, 70])
+def test_scores_of_hundreds_of_millions(G, dtype, nq):
+    """One token takes all the weight, whatever the scores' size (3.6e8: units of 2^5 in float32)."""
+    rng = np.random.default_rng(63)
+    k, v = one_ahead(900, 64, 3.0, rng)
+    k[:, 0, 1] = 6.0
+    cache, table, lens, _, vv = held(k, v)
+    q = torch.zeros((nq, 2, 64), dtype=TORCH[dtype], device=DEV)
+    q[:, :, 0] = q[:, :, 1] = 60000.0
+    for ws in (torch.empty(0, dtype=torch.uint8, device=DEV), None):
+        note("scores of 3.6e8: %s nq=%d" % (dtype, nq))
+        out = G.gvr_kv4_attention(q, cache, table, lens, 1, scale=1000.0, causal=False, workspace=ws)
+        assert np.array_equal(f64(out), np.broadcast_to(vv[7], out.shape))
