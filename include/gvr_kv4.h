@@ -87,7 +87,7 @@ gvr_status gvr_kv4_read(const gvr_kv4_cache* cache, const gvr_heads* k, const gv
  *     out = sum_t w_t v_t,  w = softmax over visible t of scale * (q . k_t)
  *     lse = log sum_t exp(scale * (q . k_t))   (natural log; -inf if none)
  * A query that sees no token gives out = 0. Masked tokens are never part of a
- * result, whatever their records hold (NaN blocks included).
+ * result, whatever their records hold (NaN blocks and infinities included).
  *
  * Numerics: the stored keys enter the matrix cores as they are, the queries as
  * sums of two 8-bit numbers (three for float16) with a common scale per 32

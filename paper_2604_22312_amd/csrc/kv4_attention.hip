@@ -176,6 +176,9 @@ DEV float weight_of(float s, float scale2, float base) {
         return __builtin_amdgcn_exp2f(__builtin_fmaf(s - base, scale2, kUp));
 }
 DEV float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+// First scale byte with codes beyond the 16-bit type (4 * 2^14; 4 * 2^126).
+template <class E>
+constexpr uint32_t kOver = __is_same(E, __bf16) ? 253 : 141;
 
 // NB bytes of codes as dwords (records are 4-byte aligned, runs of 2 bytes 2-byte).
 template <int NB>
@@ -631,11 +634,15 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
         if (!full) {
             // A masked token's weight is zero, but a NaN block times zero is
             // not: blocks that are NaN, and tokens that are not there, are
-            // taken as zeros, and the rows that see a NaN remember it.
+            // taken as zeros, and the rows that see a NaN remember it. So are,
+            // in tokens that some row does not see, blocks of values that
+            // become infinite in the 16-bit type.
+            auto first_bad = [&](int n) { return t0 + n > all_last ? kOver<E> : 255u; };
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const bool here = (there >> (16 * (j >> 2) + 4 * quarter_now + (j & 3))) & 1;
-                const bool nan = __float_as_uint(vs[j]) == 0x7F800000u;
+                const int n = 16 * (j >> 2) + 4 * quarter_now + (j & 3);
+                const bool here = (there >> n) & 1;
+                const bool nan = __float_as_uint(vs[j]) >= first_bad(n) << 23;
                 bad |= here && nan;
                 if (!here || nan) {
                     vs[j] = 0.f;
@@ -647,8 +654,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
                 const uint8_t* vsb = mine + L::kCodes + L::kScales + D / 4 * quarter / 32;
 #pragma unroll 1
                 for (int n = 0; n < kStep; ++n) {
-                    uint32_t nan = vsb[n * (D / 32)] == 255 ? 1u : 0u;
-                    if constexpr (D == 256) nan |= vsb[n * (D / 32) + 1] == 255 ? 2u : 0u;
+                    uint32_t nan = vsb[n * (D / 32)] >= first_bad(n) ? 1u : 0u;
+                    if constexpr (D == 256) nan |= vsb[n * (D / 32) + 1] >= first_bad(n) ? 2u : 0u;
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
                         nan_blocks[mt] |= ((there >> n) & 1) != 0 && t0 + n <= last[mt] ? nan : 0u;
@@ -937,6 +944,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
     // last token that this lane's row sees; that all rows of the wave see; tokens that concern the workgroup
     const int last = !live ? -1 : p.causal ? (int)(ctx - nq + qi) : ctx - 1;
     const int all_last = (int)max((int64_t)-1, p.causal ? ctx - nq + (first_row + 32 * wave) / p.group : (int64_t)ctx - 1);
+    const int wg_last = (int)max((int64_t)-1, p.causal ? ctx - nq + first_row / p.group : (int64_t)ctx - 1);
     const int wave_last_q = min((first_row + 32 * wave + 31) / p.group, shown - 1);
     const int wave_last = (first_row + 32 * wave) / p.group >= shown ? -1
                           : p.causal ? (int)max((int64_t)-1, ctx - nq + wave_last_q) : ctx - 1;   // that any row of the wave sees
@@ -991,7 +999,12 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
                                       (uint32_t)(p.kv_heads * D + (v * p.kv_heads + h) * (D / 32)));
         }
     };
-    auto stage = [&](int buf) {
+    // The first scale byte that counts as NaN in the tile whose first token is
+    // t: where some row does not see all of its tokens, that of values which are
+    // infinite in the 16-bit type (weight zero times infinity is not zero).
+    auto first_bad = [&](int t) { return t > wg_last - (M::kTile - 1) ? kOver<E> : 255u; };
+    auto stage = [&](int buf, int t) {   // the tile of first token t
+        const uint32_t bad_from = first_bad(t);
         uint8_t* base = lds + buf * M::kBytes;
 #pragma unroll
         for (int c = 0; c < M::kKPer; ++c) {
@@ -1011,7 +1024,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     // tokens that are not there, and NaN blocks (their rows get NaN in `use`), are zeros
-                    const bool here = (vthere[c] >> j) & 1, nan = vsreg[c][j] == 255u;
+                    const bool here = (vthere[c] >> j) & 1, nan = vsreg[c][j] >= bad_from;
                     bad |= here && nan;
                     if (!here || nan) vreg[c][j] = 0u, vsreg[c][j] = 127u;
                     sc[j] = scale_of(vsreg[c][j]);
@@ -1094,8 +1107,8 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
     // added or, inside a turned row, flipped.
     const int k_row = mk_place<D>(col, half);
     const int v_row = col * (2 * M::kTile), v_turn = mv_place<M::kTile>(col, half) - v_row;
-    // 32 tokens from t0, at token `tok` of the tile in `buf`.
-    auto use = [&](int buf, int tok, int t0, uint32_t there) {
+    // 32 tokens from t0, at token `tok` of the tile in `buf`; bad_from: the tile's first_bad.
+    auto use = [&](int buf, int tok, int t0, uint32_t there, uint32_t bad_from) {
         const uint8_t* kb = lds + buf * M::kBytes;
         const uint8_t* vb = kb + M::kK;
         const uint8_t* sb = vb + M::kV + (tok + col) * (D / 32);
@@ -1161,7 +1174,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
             for (int t = 0; t < 32; ++t) {
                 uint32_t nan = 0;
 #pragma unroll
-                for (int n = 0; n < D / 32; ++n) nan |= vsb[t * (D / 32) + n] == 255 ? 1u << n : 0u;
+                for (int n = 0; n < D / 32; ++n) nan |= vsb[t * (D / 32) + n] >= bad_from ? 1u << n : 0u;
                 nan_blocks |= ((there >> t) & 1) != 0 && t0 + t <= last ? nan : 0u;
             }
         }
@@ -1190,19 +1203,19 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
         lds_barrier();
         fetch(0);
         if (piece == begin) load_queries();
-        stage(0);
+        stage(0, piece);
         fetch(min(M::kTile, padded - M::kTile));
         lds_barrier();
         int buf = 0;
         for (int t = 0; t < padded; t += M::kTile) {
-            stage(buf ^ 1);
+            stage(buf ^ 1, step_at(piece, t + M::kTile));
             fetch(min(t + 2 * M::kTile, padded - M::kTile));
 #pragma unroll 1
             for (int s = 0; s < M::kTile; s += 32) {
                 const int t0 = step_at(piece, t + s);
                 if (t0 > wave_last) break;
                 const uint32_t there = (uint32_t)__ballot(slots[t + s + col] >= 0);
-                use(buf, s, t0, there);
+                use(buf, s, t0, there, first_bad(step_at(piece, t)));
             }
             lds_barrier();
             buf ^= 1;

@@ -106,3 +106,33 @@ def test_scores_of_hundreds_of_millions(G, dtype, nq):
         note("scores of 3.6e8: %s nq=%d" % (dtype, nq))
         out = G.gvr_kv4_attention(q, cache, table, lens, 1, scale=1000.0, causal=False, workspace=ws)
         assert np.array_equal(f64(out), np.broadcast_to(vv[7], out.shape))
+
+
+@pytest.mark.parametrize("dtype,huge", [("f16", 60000.0), ("bf16", 3.3e38)])
+@pytest.mark.parametrize("D,group,nq", [(64, 2, 4), (64, 5, 7), (128, 16, 3), (128, 4, 40), (256, 3, 2), (256, 2, 70), (64, 1, 140)])
+def test_masked_infinities_do_not_show(G, dtype, huge, D, group, nq):
+    """Values that the 16-bit type cannot hold (60000 is stored as 4 * 2^14, 3.3e38 as 4 * 2^126), in tokens that only
+    the later queries see: the earlier ones are right, and the later ones not finite where they see them."""
+    rng = np.random.default_rng(64)
+    n, split = 400, nq // 2
+    first = n - nq + split                      # seen by the queries from `split` on
+    k, v = rng.standard_normal((n, 1, D)), rng.standard_normal((n, 1, D))
+    v[first:, 0, 40] = huge
+    cache, table, lens, kk, vv = held(k, v)
+    assert (vv[first:, 0, 40] > (65519 if dtype == "f16" else 3.39e38)).all()
+    q = torch.from_numpy(rng.standard_normal((nq, group, D))).to(TORCH[dtype]).to(DEV)
+    u, scale = UNIT[dtype], D ** -0.5
+    for ws in (torch.empty(0, dtype=torch.uint8, device=DEV), None):
+        note("masked infinities: %s D=%d group %d nq %d %s" % (dtype, D, group, nq, "split" if ws is None else "whole"))
+        out = f64(G.gvr_kv4_attention(q, cache, table, lens, 1, workspace=ws))
+        for i in range(nq):
+            t = n - nq + i + 1
+            ref, _, mag = O.attention(f64(q)[i], kk[:t], vv[:t], scale)
+            if i < split:
+                qk = (np.abs(kk[:t, 0]) @ np.abs(f64(q)[i]).T).max()
+                eps = ((D + 8) * scale * qk + t + 64) * 2.0 ** -24
+                tol = (u + 2 * eps) * (1 + u) * mag + u * np.abs(ref) + t * 2.0 ** -40 * np.abs(vv[:t]).max() + 2.0 ** -25
+                assert (np.abs(out[i] - ref) <= tol).all(), "row %d shows a masked value" % i
+            else:
+                assert not np.isfinite(out[i][:, 40]).any(), "row %d" % i
+                assert np.isfinite(out[i][:, :32]).all()
