@@ -1386,7 +1386,7 @@ gvr_status gvr_kv4_attention(const gvr_kv4_cache* cache, const gvr_kv4_attention
     st = gvr_kv4::check_attention(*cache, a);
     if (st != GVR_OK) return st;
     if ((!workspace && ws_bytes > 0) || ((uintptr_t)workspace & 15)) return GVR_ERR_INVALID_ARG;
-    if (a.T == 0 || a.sequences == 0) return GVR_OK;
+    if (a.T == 0 || a.sequences == 0 || (a.q_start && a.max_q == 0)) return GVR_OK;
     if (!a.q || !a.out || !a.ctx_len || (!a.block_table && a.table_width > 0)) return GVR_ERR_INVALID_ARG;
     if (((uintptr_t)a.q | (uintptr_t)a.out) & 15) return GVR_ERR_INVALID_ARG;
     const gvr_kv4::AttnPlan plan = gvr_kv4::plan_attention(*cache, a, ws_bytes);

@@ -1,0 +1,38 @@
+"""Limits of the rotary and 4-bit cache entry points (no GPU): every call below
+returns before anything would be launched."""
+import ctypes
+import os
+
+import pytest
+
+vp = ctypes.c_void_p
+
+
+@pytest.fixture(scope="module")
+def K():
+    import paper_2604_22312_amd as g
+    if not os.path.exists(g.library_path()):
+        from paper_2604_22312_amd import build
+        build.build()
+    from paper_2604_22312_amd import kv4
+    kv4.lib()
+    return kv4
+
+
+def attention(lib, page=16, heads=2, D=64, pages=4, **kw):
+    a = dict(q=256, q_token_stride=256, q_head_stride=64, out=512, lse=None, block_table=64, ctx_len=64, q_start=None,
+             selection=None, T=4, table_width=8, sequences=2, max_q=0, q_heads=4, K=0, dtype=0, causal=1, scale=0.1,
+             reserved=0)
+    a.update(kw)
+    arg, c = lib._AttentionArgs(**a), lib._Cache(4096, pages, page, heads, D, 0)
+    return lib.lib().gvr_kv4_attention(ctypes.byref(c), ctypes.byref(arg), None, 0, None)
+
+
+def test_no_query_tokens_to_serve(K):
+    """max_q = 0: no sequence has a row that is served, so nothing is launched."""
+    assert attention(K, q_start=64, max_q=0) == 0
+    assert attention(K, q_start=64, max_q=0, selection=64, K=5) == 0
+    n = ctypes.c_size_t(7)
+    arg = K._AttentionArgs(q_start=64, T=4, table_width=8, sequences=2, q_heads=4, scale=0.1)
+    assert K.lib().gvr_kv4_attention_workspace(ctypes.byref(K._Cache(4096, 4, 16, 2, 64, 0)), ctypes.byref(arg),
+                                               ctypes.byref(n)) == 0 and n.value == 0
