@@ -252,6 +252,7 @@ def _attention_args(q, cache, block_table, ctx_len, kv_heads, selection, q_start
         _index(q_start, "q_start", torch.int32, (B + 1,), dev)
         max_q = T if max_q is None else int(max_q)
         _need(0 <= max_q, "max_q must not be negative")
+        max_q = min(max_q, T)   # (an int32 in the C call)
     else:
         _need(T % B == 0 if B else T == 0, "without q_start every sequence has as many query tokens")
         max_q = T // B if B else 0

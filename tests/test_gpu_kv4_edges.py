@@ -136,3 +136,17 @@ def test_masked_infinities_do_not_show(G, dtype, huge, D, group, nq):
             else:
                 assert not np.isfinite(out[i][:, 40]).any(), "row %d" % i
                 assert np.isfinite(out[i][:, :32]).all()
+
+
+@pytest.mark.parametrize("max_q", [0, 3, 9, 2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 1])
+def test_max_q_of_any_size(G, max_q):
+    """At most max_q query tokens of a sequence are served, however large it is."""
+    rng = np.random.default_rng(65)
+    cache, table, lens, _, _ = held(rng.standard_normal((50, 1, 64)), rng.standard_normal((50, 1, 64)))
+    q = torch.randn((9, 4, 64), device=DEV).bfloat16()
+    start = torch.tensor([0, 9], dtype=torch.int32, device=DEV)
+    note("max_q = %d" % max_q)
+    want = G.gvr_kv4_attention(q, cache, table, lens, 1)
+    out = G.gvr_kv4_attention(q, cache, table, lens, 1, q_start=start, max_q=max_q, out=torch.full_like(q, 3.0))
+    served = min(max_q, 9)
+    assert (out[served:] == 3).all() and torch.equal(out[:served], want[:served])
