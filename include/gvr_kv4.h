@@ -135,7 +135,8 @@ gvr_status gvr_kv4_attention_workspace(const gvr_kv4_cache* cache, const gvr_kv4
  * asks for lowers the split, NULL with 0 bytes runs unsplit.
  * Errors: GVR_ERR_INVALID_ARG (a NULL or misaligned required pointer, bad
  * sizes, heads, dtype, or a workspace NULL with bytes), GVR_ERR_TOO_LONG
- * (table_width * page_size, T or the grid above 2^31 - 16), GVR_ERR_HIP.
+ * (table_width * page_size or T above 2^31 - 16, or a grid of 2^32 threads or
+ * more), GVR_ERR_HIP.
  * T == 0, sequences == 0 or max_q == 0 with q_start is a no-op. */
 gvr_status gvr_kv4_attention(const gvr_kv4_cache* cache, const gvr_kv4_attention_args* args, void* workspace,
                              size_t ws_bytes, void* stream);

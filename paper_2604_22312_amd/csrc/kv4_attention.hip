@@ -872,7 +872,7 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
 // one's rows are then empty.
 template <int D, int NW>
 struct Many {
-    static constexpr int kThreads = 64 * NW;
+    static constexpr int kThreads = 64 * NW;               // (AttnPlan::threads)
     static constexpr int kTile = 16 * NW;                  // tokens
     static constexpr int kK = kTile * D / 2;               // bytes: codes of K
     static constexpr int kV = kTile * D * 2;               // V
@@ -1264,7 +1264,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
 // order, `kAt` at a time. The weights are made first, so that the loads of the
 // parts wait for nothing.
 template <class E, int D>
-__global__ __launch_bounds__(256) void combine_kernel(AttnParams p) {
+__global__ __launch_bounds__(gvr_kv4::kJoinThreads) void combine_kernel(AttnParams p) {
     constexpr int kPer = D / 4;            // threads of a split: four dimensions each
     constexpr int kAt = 256 / kPer;        // splits at a time
     __shared__ float4 acc_l[256];
@@ -1351,8 +1351,8 @@ gvr_status launch(const AttnParams& p, int64_t jobs, void* stream) {
     }
     if (hipGetLastError() != hipSuccess) return GVR_ERR_HIP;
     if (p.splits > 1 || p.balanced) {
-        hipLaunchKernelGGL((combine_kernel<E, D>), dim3((unsigned)((int64_t)p.sequences * p.max_q * p.q_heads)), dim3(256),
-                           0, (hipStream_t)stream, p);
+        hipLaunchKernelGGL((combine_kernel<E, D>), dim3((unsigned)((int64_t)p.sequences * p.max_q * p.q_heads)),
+                           dim3(gvr_kv4::kJoinThreads), 0, (hipStream_t)stream, p);
         if (hipGetLastError() != hipSuccess) return GVR_ERR_HIP;
     }
     return GVR_OK;
@@ -1390,8 +1390,7 @@ gvr_status gvr_kv4_attention(const gvr_kv4_cache* cache, const gvr_kv4_attention
     if (!a.q || !a.out || !a.ctx_len || (!a.block_table && a.table_width > 0)) return GVR_ERR_INVALID_ARG;
     if (((uintptr_t)a.q | (uintptr_t)a.out) & 15) return GVR_ERR_INVALID_ARG;
     const gvr_kv4::AttnPlan plan = gvr_kv4::plan_attention(*cache, a, ws_bytes);
-    if (plan.jobs > gvr_kv4::kMaxCount || (int64_t)a.sequences * plan.max_q * a.q_heads > gvr_kv4::kMaxCount)
-        return GVR_ERR_TOO_LONG;
+    if (plan.jobs > gvr_kv4::kMaxThreads / plan.threads) return GVR_ERR_TOO_LONG;
     AttnParams p;
     p.cache = cache->data;
     p.q = a.q, p.qt = a.q_token_stride, p.qh = a.q_head_stride;

@@ -53,6 +53,9 @@ constexpr int kRows = 16;          // query rows of a wave
 constexpr int kStep = 32;          // tokens of a wave's step
 constexpr int kWaves = 8;          // of a workgroup
 constexpr int kThreads = 64 * kWaves;
+constexpr int kJoinThreads = 256;  // of the kernel that joins a row's and head's splits (plans that split have
+                                   // few workgroups and so few rows: its launch always fits)
+constexpr int64_t kMaxThreads = 0xFFFFFFFF;   // of a launch
 constexpr int kMaxSplits = 1024;
 constexpr int kMaxBalanced = 2048;  // sequences whose lengths a workgroup adds up
 // The model of plan_attention, in tiles' times.
@@ -81,6 +84,7 @@ struct AttnPlan {
     int hw_shift;     // log2 of the KV heads of a workgroup
     int tw_shift;     // log2 of the waves that share a head's steps
     int64_t jobs;     // workgroups
+    int threads;      // of one
     int splits;       // of a context or selection
     int chunk;        // tokens of a split
     bool balanced;    // few rows: the kernel sizes the splits by the contexts' lengths, `units` in all
@@ -107,6 +111,7 @@ inline AttnPlan plan_attention(const gvr_kv4_cache& c, const gvr_kv4_attention_a
     const int64_t together = a.selection ? G : (int64_t)p.max_q * G;
     p.row_tiles = together > kRows && c.head_dim != 256 ? 2 : 1;
     const int rows = p.many ? rows_wg : p.row_tiles * kRows;
+    p.threads = p.many ? 2 * rows_wg : kThreads;
     const int64_t tiles = a.selection ? (int64_t)p.max_q * ((G + rows - 1) / rows) : (together + rows - 1) / rows;
     p.tiles = (int)(tiles > kMaxCount ? kMaxCount : tiles);
     const int64_t n = a.selection ? a.K : a.table_width * c.page_size;

@@ -36,3 +36,12 @@ def test_no_query_tokens_to_serve(K):
     arg = K._AttentionArgs(q_start=64, T=4, table_width=8, sequences=2, q_heads=4, scale=0.1)
     assert K.lib().gvr_kv4_attention_workspace(ctypes.byref(K._Cache(4096, 4, 16, 2, 64, 0)), ctypes.byref(arg),
                                                ctypes.byref(n)) == 0 and n.value == 0
+
+
+def test_more_threads_than_a_launch_holds(K):
+    """2^23 workgroups of 512 threads (2^24 of 256 at D = 256): refused before the launch."""
+    far = dict(q_start=64, pages=1000)
+    assert attention(K, selection=64, K=2048, sequences=1024, T=16384, max_q=16384, **far) == -5
+    assert attention(K, selection=64, K=5, sequences=1, T=1 << 23, max_q=1 << 23, heads=8, q_heads=8, **far) == -5
+    assert attention(K, sequences=1 << 14, T=1 << 19, max_q=1 << 19, **far) == -5
+    assert attention(K, sequences=1 << 13, T=1 << 19, max_q=1 << 19, D=256, **far) == -5
