@@ -132,16 +132,15 @@ __global__ __launch_bounds__(kBlock) void rotate_any_kernel(RotParams p) {
 }
 
 // Table: a workgroup's first R/2 threads hold the angles in LDS, then each
-// thread makes pairs of kTableRows positions.
-constexpr int kTableRows = 64;
-__global__ __launch_bounds__(gvr_yarn::kMaxPairs) void rope_table_kernel(int64_t n, gvr_yarn::RopeArgs a, double gain,
-                                                                         float* __restrict__ table) {
+// thread makes pairs of `rows` positions.
+__global__ __launch_bounds__(gvr_yarn::kMaxPairs) void rope_table_kernel(int64_t n, int rows, gvr_yarn::RopeArgs a,
+                                                                         double gain, float* __restrict__ table) {
     __shared__ double th[gvr_yarn::kMaxPairs];
     const int half = a.d / 2;
     if ((int)threadIdx.x < half) th[threadIdx.x] = gvr_yarn::yarn_angle(threadIdx.x, a);
     __syncthreads();
-    const int64_t p0 = (int64_t)blockIdx.x * kTableRows;
-    const int items = (int)(n - p0 < kTableRows ? n - p0 : kTableRows) * half;
+    const int64_t p0 = (int64_t)blockIdx.x * rows;
+    const int items = (int)(n - p0 < rows ? n - p0 : rows) * half;
     for (int i = threadIdx.x; i < items; i += gvr_yarn::kMaxPairs) {
         const int64_t pos = p0 + i / half;
         const int pair = i % half;
@@ -182,8 +181,9 @@ gvr_status gvr_rope_table(int64_t n, const gvr_rope_params* params, double gain,
     if (n < 0 || !isfinite(gain) || (n > 0 && !table) || ((uintptr_t)table & 7)) return GVR_ERR_INVALID_ARG;
     if (n > gvr_rot::kMaxCount) return GVR_ERR_TOO_LONG;
     if (n == 0) return GVR_OK;
-    hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)((n + kTableRows - 1) / kTableRows)),
-                       dim3(gvr_yarn::kMaxPairs), 0, (hipStream_t)stream, n, a, gain, table);
+    const int rows = gvr_rot::table_rows(n);
+    hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)((n + rows - 1) / rows)), dim3(gvr_yarn::kMaxPairs), 0,
+                       (hipStream_t)stream, n, rows, a, gain, table);
     return hipGetLastError() == hipSuccess ? GVR_OK : GVR_ERR_HIP;
 }
 

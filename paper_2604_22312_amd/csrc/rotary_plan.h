@@ -15,6 +15,10 @@ constexpr int64_t kMaxCount = ((int64_t)1 << 31) - 16;
 constexpr int kBlock = 256;
 constexpr int64_t kMaxRows = 65535;   // of a launch (blockIdx.y)
 
+// Positions of a workgroup (256 threads) that makes the table: 64, or more where
+// a launch's threads would not fit 32 bits (2^30 - 64 positions and more).
+inline int table_rows(int64_t n) { return n <= (int64_t)1 << 29 ? 64 : 256; }
+
 inline int dtype_size(int dtype) { return dtype == GVR_F32 ? 4 : (dtype == GVR_BF16 || dtype == GVR_F16) ? 2 : 0; }
 
 // Rows that 16-byte accesses at multiples of 8 elements can serve.

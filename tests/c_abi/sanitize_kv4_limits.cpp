@@ -51,6 +51,12 @@ int main() {
         }
     }
     CHECK(split > 1000 && many > 1000 && beyond > 1000);
+    for (int i = 0; i < 100000; ++i) {   // workgroups of 256 threads that make the rotary table
+        const int64_t n = i == 0 ? gvr_rot::kMaxCount : pick(1, (int64_t)1 << pick(0, 31));
+        if (n > gvr_rot::kMaxCount) continue;
+        const int64_t rows = gvr_rot::table_rows(n);
+        CHECK((n + rows - 1) / rows * 256 <= kMaxThreads && rows * 256 < (1 << 24));
+    }
     std::puts("ok");
     return 0;
 }
