@@ -110,6 +110,27 @@ def _stream(stream, device):
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
+def _new(shape, dtype, dev, stream, returned=True):
+    """A tensor that a call on ``stream`` writes. torch's allocator hands out a
+    block in the order of the stream that is current: on another one the call
+    could write it before work that still reads the block it was. So it comes
+    from ``stream``'s own pool, and goes back there (``returned``: the caller
+    gets it) when the current stream, too, is through with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    current = torch.cuda.current_stream(dev)
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+        stream = torch.cuda.ExternalStream(handle, device=dev) if handle else torch.cuda.default_stream(dev)
+    if stream.cuda_stream == current.cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=dev)
+    if returned:
+        t.record_stream(current)
+    return t
+
+
 def _on_device(dev):
     """The tensors' device made current for the call (a no-op context when it
     already is, which skips the device switch and restore)."""

@@ -9,7 +9,7 @@ import ctypes
 import torch
 
 from . import binding
-from .binding import GvrError, PreparedCall, RopeParams, _on_device, _ptr, _rope_args, _stream
+from .binding import GvrError, PreparedCall, RopeParams, _new, _on_device, _ptr, _rope_args, _stream
 
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 ROPE_INTERLEAVED, ROPE_TRANSPOSED = 1, 2
@@ -126,7 +126,7 @@ def gvr_rope_table(n, params=None, gain=1.0, device="cuda", out=None, stream=Non
     n = int(n)
     shape = (max(n, 0), max(params.d_rope, 0) // 2, 2)
     if out is None:
-        out = torch.empty(shape, dtype=torch.float32, device=dev)
+        out = _new(shape, torch.float32, dev, stream)
     else:
         _index(out, "out", torch.float32, shape, dev)
     with _on_device(dev):
@@ -145,7 +145,7 @@ def prepare_gvr_rope_rotate(x, positions, table, interleaved=False, inverse=Fals
     _index(positions, "positions", torch.int32, (T,), dev)
     cs = _cs(table, interleaved, inverse, D, dev)
     if out is None:
-        out = torch.empty((T, H, D), dtype=x.dtype, device=dev)
+        out = _new((T, H, D), x.dtype, dev, stream)
     os = _heads_tensor(_no_overlap(out, "out"), "out", x.dtype, x.shape, dev)
     args = (ctypes.byref(xs), ctypes.byref(os), DTYPES[x.dtype], T, H, D, _ptr(positions), ctypes.byref(cs),
             _stream(stream, dev))
@@ -220,8 +220,8 @@ def prepare_gvr_kv4_read(cache, slots, kv_heads, head_dim, dtype=torch.bfloat16,
     T = slots.shape[0]
     _index(slots, "slots", torch.int64, (T,), dev)
     shape = (T, c.kv_heads, c.head_dim)
-    k = torch.empty(shape, dtype=dtype, device=dev) if k is None else k
-    v = torch.empty(shape, dtype=dtype, device=dev) if v is None else v
+    k = _new(shape, dtype, dev, stream) if k is None else k
+    v = _new(shape, dtype, dev, stream) if v is None else v
     ks = _heads_tensor(_no_overlap(k, "k"), "k", dtype, shape, dev)
     vs = _heads_tensor(_no_overlap(v, "v"), "v", dtype, shape, dev)
     args = (ctypes.byref(c), ctypes.byref(ks), ctypes.byref(vs), DTYPES[dtype], T, _ptr(slots), _stream(stream, dev))
@@ -234,7 +234,8 @@ def gvr_kv4_read(cache, slots, kv_heads, head_dim, dtype=torch.bfloat16, k=None,
     return prepare_gvr_kv4_read(cache, slots, kv_heads, head_dim, dtype, k, v, stream)()
 
 
-def _attention_args(q, cache, block_table, ctx_len, kv_heads, selection, q_start, max_q, causal, scale, out, lse):
+def _attention_args(q, cache, block_table, ctx_len, kv_heads, selection, q_start, max_q, causal, scale, out, lse,
+                    stream=None):
     _heads_tensor(q, "q")
     _need(q.dtype != torch.float32, "q must be bfloat16 or float16")
     T, H, D = q.shape
@@ -263,7 +264,7 @@ def _attention_args(q, cache, block_table, ctx_len, kv_heads, selection, q_start
         K = selection.shape[1]
         _index(selection, "selection", torch.int32, (T, K), dev)
     if out is None:
-        out = torch.empty((T, H, D), dtype=q.dtype, device=dev)
+        out = _new((T, H, D), q.dtype, dev, stream)
     else:
         _index(out, "out", q.dtype, (T, H, D), dev)
     if lse is not None:
@@ -295,7 +296,7 @@ def prepare_gvr_kv4_attention(q, cache, block_table, ctx_len, kv_heads, selectio
                               causal=True, scale=None, out=None, lse=None, workspace=None, stream=None):
     """A ``PreparedOp`` of ``gvr_kv4_attention`` (it keeps the workspace)."""
     a, c, out = _attention_args(q, cache, block_table, ctx_len, kv_heads, selection, q_start, max_q, causal, scale, out,
-                                lse)
+                                lse, stream)
     dev = q.device
     if workspace is None:
         n = ctypes.c_size_t(0)
@@ -303,10 +304,7 @@ def prepare_gvr_kv4_attention(q, cache, block_table, ctx_len, kv_heads, selectio
             st = lib().gvr_kv4_attention_workspace(ctypes.byref(c), ctypes.byref(a), ctypes.byref(n))
         if st != 0:
             raise GvrError("gvr_kv4_attention_workspace", st)
-        workspace = torch.empty(max(int(n.value), 1), dtype=torch.uint8, device=dev)
-        if stream is not None:
-            workspace.record_stream(stream if isinstance(stream, torch.cuda.Stream)
-                                    else torch.cuda.ExternalStream(int(stream), device=dev))
+        workspace = _new(max(int(n.value), 1), torch.uint8, dev, stream, returned=False)
     _need(isinstance(workspace, torch.Tensor) and workspace.device == dev and workspace.is_contiguous()
           and workspace.data_ptr() % 16 == 0, "workspace must be a contiguous 16-byte aligned tensor on %s" % dev)
     nbytes = workspace.numel() * workspace.element_size()
