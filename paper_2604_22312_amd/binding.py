@@ -151,7 +151,7 @@ class _NoSwitch:
 _NO_SWITCH = _NoSwitch()
 
 
-def _check(scores, row_len, prev_topk, K, out_idx):
+def _check(scores, row_len, prev_topk, K, out_idx, stream=None):
     if not isinstance(scores, torch.Tensor) or scores.dtype != torch.float32 or scores.dim() != 2:
         raise ValueError("scores must be a float32 tensor [B][ld]")
     if not scores.is_cuda:
@@ -169,7 +169,7 @@ def _check(scores, row_len, prev_topk, K, out_idx):
                 or not prev_topk.is_contiguous()):
             raise ValueError("prev_topk must be a contiguous int32 tensor [B][K] on the scores' device")
     if out_idx is None:
-        out_idx = torch.empty((B, max(K, 0)), dtype=torch.int32, device=dev)
+        out_idx = _new((B, max(K, 0)), torch.int32, dev, stream)
     elif (out_idx.dtype != torch.int32 or out_idx.shape != (B, K) or out_idx.device != dev
           or not out_idx.is_contiguous()):
         raise ValueError("out_idx must be a contiguous int32 tensor [B][K] on the scores' device")
@@ -177,7 +177,7 @@ def _check(scores, row_len, prev_topk, K, out_idx):
 
 
 def _call(fn_name, scores, row_len, prev_topk, K, out_idx, stream):
-    B, ld, K, out_idx = _check(scores, row_len, prev_topk, K, out_idx)
+    B, ld, K, out_idx = _check(scores, row_len, prev_topk, K, out_idx, stream)
     with _on_device(scores.device):
         st = getattr(lib(), fn_name)(_ptr(scores), B, ld, _ptr(row_len), _ptr(prev_topk), K,
                                      _ptr(out_idx), _stream(stream, scores.device))
@@ -197,7 +197,7 @@ def radix_topk(scores, row_len, prev_topk, K, out_idx=None, stream=None):
 
 
 def _call_ex(radix, scores, row_len, prev_topk, K, out_idx, stream, options, stats, fn="gvr_topk_ex"):
-    B, ld, K, out_idx = _check(scores, row_len, prev_topk, K, out_idx)
+    B, ld, K, out_idx = _check(scores, row_len, prev_topk, K, out_idx, stream)
     if stats is not None and (stats.dtype != torch.int32 or stats.shape != (B, STATS_INTS)
                               or stats.device != scores.device or not stats.is_contiguous()):
         raise ValueError("stats must be a contiguous int32 tensor [B][%d] on the scores' device" % STATS_INTS)
@@ -265,7 +265,7 @@ def new_workspace(B, ld, K, use_guess=True, options=None, device=None):
 
 
 def _call_ws(radix, scores, row_len, prev_topk, K, workspace, out_idx, stream, options, stats):
-    B, ld, K, out_idx = _check(scores, row_len, None if radix else prev_topk, K, out_idx)
+    B, ld, K, out_idx = _check(scores, row_len, None if radix else prev_topk, K, out_idx, stream)
     if stats is not None and (stats.dtype != torch.int32 or stats.shape != (B, STATS_INTS)
                               or stats.device != scores.device or not stats.is_contiguous()):
         raise ValueError("stats must be a contiguous int32 tensor [B][%d] on the scores' device" % STATS_INTS)
@@ -323,7 +323,7 @@ class PreparedCall:
 
 
 def _prepare(radix, scores, row_len, prev_topk, K, out_idx, stream, options, workspace=None):
-    B, ld, K, out_idx = _check(scores, row_len, None if radix else prev_topk, K, out_idx)
+    B, ld, K, out_idx = _check(scores, row_len, None if radix else prev_topk, K, out_idx, stream)
     L = lib()
     opt = None
     if options is not None:
@@ -426,7 +426,7 @@ def gvr_rope_g(n, params=None, device="cuda", g=None, theta=None, stream=None):
     params, dev = _rope_args(params, device)
     n = int(n)
     if g is None:
-        g = torch.empty(max(n, 0), dtype=torch.float64, device=dev)
+        g = _new(max(n, 0), torch.float64, dev, stream)
     for t, size in ((g, n), (theta, params.d_rope // 2)):
         if t is not None and (t.dtype != torch.float64 or t.numel() != size or t.device != dev
                               or not t.is_contiguous()):
@@ -444,11 +444,11 @@ def gvr_rope_prior(n, K, params=None, device="cuda", out=None, g=None, stream=No
     params, dev = _rope_args(params, device)
     n, K = int(n), int(K)
     if g is None:
-        g = torch.empty(max(n, 0), dtype=torch.float64, device=dev)
+        g = _new(max(n, 0), torch.float64, dev, stream)
     elif g.dtype != torch.float64 or g.numel() != n or g.device != dev or not g.is_contiguous():
         raise ValueError("g must be a contiguous float64 tensor of n elements on the device")
     if out is None:
-        out = torch.empty(max(K, 0), dtype=torch.int32, device=dev)
+        out = _new(max(K, 0), torch.int32, dev, stream)
     elif out.dtype != torch.int32 or out.numel() != K or out.device != dev or not out.is_contiguous():
         raise ValueError("out must be a contiguous int32 tensor of K elements on the device")
     with _on_device(dev):
@@ -458,7 +458,7 @@ def gvr_rope_prior(n, K, params=None, device="cuda", out=None, g=None, stream=No
     return out
 
 
-def _check_indexer(q, w, k, k_scale, row_len, scores):
+def _check_indexer(q, w, k, k_scale, row_len, scores, stream):
     for name, t, dt in (("q", q, torch.uint8), ("w", w, torch.float32), ("k", k, torch.uint8),
                         ("k_scale", k_scale, torch.float32)):
         if not isinstance(t, torch.Tensor) or t.dtype != dt or not t.is_cuda or not t.is_contiguous():
@@ -478,7 +478,7 @@ def _check_indexer(q, w, k, k_scale, row_len, scores):
                                 or not row_len.is_contiguous()):
         raise ValueError("row_len must be a contiguous int32 tensor [B] on the device")
     if scores is None:
-        scores = torch.empty((B, ld), dtype=torch.float32, device=dev)
+        scores = _new((B, ld), torch.float32, dev, stream)
     elif (scores.dtype != torch.float32 or scores.shape != (B, ld) or scores.device != dev
           or not scores.is_contiguous()):
         raise ValueError("scores must be a contiguous float32 tensor [B][ld] on the device")
@@ -489,7 +489,7 @@ def gvr_indexer_scores(q, w, k, k_scale, row_len=None, scores=None, stream=None)
     """Indexer scores I [B][ld] (float32; entries s >= n_b are not written)
     from FP8 E4M3 bytes q [B][H][D], key cache k [C][ld][D] shared by B / C
     consecutive rows, k_scale [C][ld] and head weights w [B][H]."""
-    B, H, D, group, ld, scores = _check_indexer(q, w, k, k_scale, row_len, scores)
+    B, H, D, group, ld, scores = _check_indexer(q, w, k, k_scale, row_len, scores, stream)
     with _on_device(q.device):
         st = lib().gvr_indexer_scores(_ptr(q), _ptr(w), _ptr(k), _ptr(k_scale), B, H, D, group, ld,
                                       _ptr(row_len), _ptr(scores), _stream(stream, q.device))
@@ -501,8 +501,8 @@ def gvr_indexer_scores(q, w, k, k_scale, row_len=None, scores=None, stream=None)
 def gvr_indexer_topk(q, w, k, k_scale, row_len, prev_topk, K, scores=None, out_idx=None, stream=None,
                      options=None, stats=None):
     """The indexer, then gvr_topk_ex on its scores; returns (out_idx [B][K], scores [B][ld])."""
-    B, H, D, group, ld, scores = _check_indexer(q, w, k, k_scale, row_len, scores)
-    _, _, K, out_idx = _check(scores, row_len, prev_topk, K, out_idx)
+    B, H, D, group, ld, scores = _check_indexer(q, w, k, k_scale, row_len, scores, stream)
+    _, _, K, out_idx = _check(scores, row_len, prev_topk, K, out_idx, stream)
     opt = None
     if options is not None:
         opt = Options(**options) if isinstance(options, dict) else options
@@ -529,7 +529,7 @@ def gvr_read_floor(scores, row_len=None, out_words=None, stream=None):
                                 or row_len.device != scores.device or not row_len.is_contiguous()):
         raise ValueError("row_len must be a contiguous int32 tensor [B] on the scores' device")
     if out_words is None:
-        out_words = torch.empty((B, 16), dtype=torch.int32, device=scores.device)
+        out_words = _new((B, 16), torch.int32, scores.device, stream)
     elif (out_words.dtype != torch.int32 or out_words.shape != (B, 16) or out_words.device != scores.device
           or not out_words.is_contiguous()):
         raise ValueError("out_words must be a contiguous int32 tensor [B][16] on the scores' device")

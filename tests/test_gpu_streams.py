@@ -1,5 +1,4 @@
-"""Tensors that the rotary and 4-bit cache calls make for a given stream belong to
-that stream: torch's allocator orders a block's uses by the stream that it was
+"""Tensors that a call makes for a given stream belong to that stream: torch's allocator orders a block's uses by the stream that it was
 allocated on, so a block of another stream could still be in use there."""
 import pytest
 import torch
@@ -57,3 +56,22 @@ def test_made_tensors_belong_to_the_stream(G, kind):
                           ("workspace", workspace)):
             assert owner(ptr) == want, name
         assert torch.equal(out, call.out) and torch.equal(out, G.gvr_kv4_attention(q, cache, tab, lens, 2))
+
+
+def test_made_tensors_of_the_selection_belong_to_the_stream(G):
+    s, side = torch.cuda.Stream(), torch.cuda.Stream()
+    scores = torch.randn((3, 5000), device=DEV)
+    q = torch.zeros((3, 64, 128), dtype=torch.uint8, device=DEV)
+    w, k, ks = torch.ones((3, 64), device=DEV), torch.zeros((3, 300, 128), dtype=torch.uint8, device=DEV), torch.ones((3, 300), device=DEV)
+    lens = torch.full((3,), 300, dtype=torch.int32, device=DEV)
+    note("streams: selection")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        made = [G.gvr_topk(scores, None, None, 2048, stream=s), G.radix_topk(scores, None, None, 2048, stream=s),
+                G.gvr_topk_ex(scores, None, None, 2048, stream=s), G.prepare_gvr_topk(scores, None, None, 2048, stream=s)(),
+                G.gvr_rope_g(5000, device=DEV, stream=s), G.gvr_rope_prior(5000, 2048, device=DEV, stream=s),
+                G.gvr_indexer_scores(q, w, k, ks, lens, stream=s), *G.gvr_indexer_topk(q, w, k, ks, lens, None, 100, stream=s)]
+        torch.cuda.synchronize()
+        for i, t in enumerate(made):
+            assert owner(t.data_ptr()) == s.cuda_stream, i
+        assert torch.equal(made[0], made[1]) and torch.equal(made[0], made[2]) and torch.equal(made[0], made[3])
