@@ -137,7 +137,8 @@ def gvr_rope_table(n, params=None, gain=1.0, device="cuda", out=None, stream=Non
 
 
 def prepare_gvr_rope_rotate(x, positions, table, interleaved=False, inverse=False, out=None, stream=None):
-    """A ``PreparedOp`` of ``gvr_rope_rotate``."""
+    """A ``PreparedOp`` of ``gvr_rope_rotate``. Its calls write the same tensor
+    again and are not seen by autograd."""
     xs = _heads_tensor(x, "x")
     T, H, D = x.shape
     dev = x.device
@@ -152,13 +153,53 @@ def prepare_gvr_rope_rotate(x, positions, table, interleaved=False, inverse=Fals
     return _prepared("gvr_rope_rotate", dev, args, out, (x, positions, table, xs, os, cs, stream))
 
 
+class _Rotate(torch.autograd.Function):
+    """The rotation as a node of the graph; ``out`` (x itself or another tensor)
+    is written in place. Linear, so its gradient is the transposed rotation."""
+
+    @staticmethod
+    def forward(ctx, x, out, positions, table, interleaved, inverse, stream):
+        ctx.save_for_backward(positions, table)
+        ctx.how = (interleaved, not inverse)
+        if out is not None:
+            ctx.mark_dirty(out)
+        return prepare_gvr_rope_rotate(x, positions, table, interleaved, inverse, out, stream)()
+
+    @staticmethod
+    def backward(ctx, grad):
+        positions, table = ctx.saved_tensors
+        grad = grad if grad.stride(2) == 1 else grad.contiguous()   # (a sum's gradient is one element)
+        return (gvr_rope_rotate(grad, positions, table, *ctx.how),) + (None,) * 6
+
+
+class _RotateInPlace(_Rotate):
+    @staticmethod
+    def forward(ctx, x, positions, table, interleaved, inverse, stream):
+        return _Rotate.forward(ctx, x, x, positions, table, interleaved, inverse, stream)
+
+    @staticmethod
+    def backward(ctx, grad):
+        return _Rotate.backward(ctx, grad)[:6]
+
+
 def gvr_rope_rotate(x, positions, table, interleaved=False, inverse=False, out=None, stream=None):
     """x [T][H][D] (bfloat16, float16 or float32; any token and head stride)
     with the first 2 * table.shape[1] elements of each head rotated to its
     token's position (int32 [T]). ``interleaved``: pairs (2i, 2i+1) instead of
     (i, i + rot/2). ``inverse``: the transposed rotation, which takes the
-    gradient of the result to the gradient of x. ``out`` may be ``x``."""
-    return prepare_gvr_rope_rotate(x, positions, table, interleaved, inverse, out, stream)()
+    gradient of the result to the gradient of x. ``out`` may be ``x``. While
+    gradients are recorded the call is a node of x's graph (the table gets no
+    gradient)."""
+    if torch.is_grad_enabled() and isinstance(x, torch.Tensor) and (x.requires_grad or getattr(out, "requires_grad", False)):
+        _need(not isinstance(out, torch.Tensor) or not (out.is_leaf and out.requires_grad),
+              "out is a leaf that requires a gradient: write into it under torch.no_grad()")
+        if out is x:
+            return _RotateInPlace.apply(x, positions, table, interleaved, inverse, stream)
+        return _Rotate.apply(x, out, positions, table, interleaved, inverse, stream)
+    y = prepare_gvr_rope_rotate(x, positions, table, interleaved, inverse, out, stream)()
+    if out is not None and not out.is_inference():
+        torch.autograd.graph.increment_version(out)   # (a graph may have saved it)
+    return y
 
 
 def gvr_kv4_record_bytes(kv_heads, head_dim) -> int:

@@ -33,3 +33,89 @@ def test_table_of_more_than_2_30_positions(G):
     ref = np.stack([np.cos(phase), np.sin(phase)], axis=-1)
     # float64's own unit of the phase (2^30 * 2^-52), and one rounding to float32
     assert np.abs(got - ref).max() <= 2.0 ** -24 + 2.0 ** -21
+
+
+# ---- gradients through autograd
+
+def rotary(rng, T=9, H=3, D=48, rot=40, dtype="f32", gain=1.2, P=100):
+    tab = O.rope_table(P, rot, gain).astype(np.float32)
+    pos = rng.integers(0, P, T).astype(np.int32)
+    x, g = (torch.from_numpy(rng.standard_normal((T, H, D))).to(TORCH[dtype]).to(DEV) for _ in range(2))
+    return x, g, torch.from_numpy(pos).to(DEV), torch.from_numpy(tab).to(DEV), pos, tab
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("inv", [False, True])
+def test_backward(G, dtype, inter, inv):
+    """The gradient is the transposed rotation of the result's, bit for bit, and the formula's."""
+    x, g, pos, tab, pn, tn = rotary(np.random.default_rng(71), dtype=dtype)
+    x.requires_grad_()
+    y = G.gvr_rope_rotate(x, pos, tab, inter, inv)
+    assert y.requires_grad and torch.equal(y.detach(), G.gvr_rope_rotate(x.detach(), pos, tab, inter, inv))
+    y.backward(g)
+    assert torch.equal(x.grad, G.gvr_rope_rotate(g, pos, tab, inter, not inv))
+    want = O.rotate(g.cpu().float().numpy(), pn, tn, inter, not inv)
+    assert torch.equal(x.grad.cpu(), torch.from_numpy(want).to(TORCH[dtype]))
+
+
+def test_backward_against_differences(G):
+    """sum(w * rotate(x)): the gradient against difference quotients (linear: exact up to rounding of float32 products
+    and sums of |x| <= 6, as in the gradient's other test)."""
+    x, w, pos, tab, _, _ = rotary(np.random.default_rng(72))
+    x.requires_grad_()
+    (w * G.gvr_rope_rotate(x, pos, tab)).sum().backward()
+    base = f64(G.gvr_rope_rotate(x.detach(), pos, tab))
+    for j in (0, 3, 19, 20, 39, 40, 47):
+        step = x.detach().clone()
+        step[:, 1, j] += 1.0
+        moved = (f64(G.gvr_rope_rotate(step, pos, tab)) - base) / (f64(step) - f64(x))[:, 1, j][:, None, None]
+        assert np.abs((moved * f64(w)).sum(axis=(1, 2)) - f64(x.grad)[:, 1, j]).max() <= 8 * 60 * 2.0 ** -24
+
+
+def test_backward_of_layouts(G):
+    """Gradients that are one element expanded (a sum's), strided inputs, and a second derivative."""
+    x, g, pos, tab, _, _ = rotary(np.random.default_rng(73))
+    wide = torch.randn((9, 5, 60), device=DEV, requires_grad=True)
+    G.gvr_rope_rotate(wide[:, 1:4, 3:51], pos, tab).sum().backward()
+    want = torch.zeros_like(wide)
+    want[:, 1:4, 3:51] = G.gvr_rope_rotate(torch.ones_like(x), pos, tab, inverse=True)
+    assert torch.equal(wide.grad, want)
+    x.requires_grad_()
+    g.requires_grad_()
+    gx, = torch.autograd.grad(G.gvr_rope_rotate(x, pos, tab), x, g, create_graph=True)
+    gg, = torch.autograd.grad(gx, g, x.detach())
+    assert torch.equal(gg, G.gvr_rope_rotate(x.detach(), pos, tab))
+
+
+def test_out_and_autograd(G):
+    """Written in place, into another tensor, and without gradients."""
+    x, g, pos, tab, _, _ = rotary(np.random.default_rng(74))
+    want = G.gvr_rope_rotate(g, pos, tab, inverse=True)
+    for other in (False, True):
+        leaf = x.clone().requires_grad_()
+        y = leaf * 2.0
+        out = torch.empty_like(x) if other else y
+        z = G.gvr_rope_rotate(y, pos, tab, out=out)
+        assert z is out and z.requires_grad and torch.equal(z.detach(), G.gvr_rope_rotate(2.0 * x, pos, tab))
+        z.backward(g)
+        assert torch.equal(leaf.grad, 2.0 * want)
+    leaf = x.clone().requires_grad_()
+    with pytest.raises(ValueError):
+        G.gvr_rope_rotate(x, pos, tab, out=leaf)
+    with pytest.raises(ValueError):
+        G.gvr_rope_rotate(leaf, pos, tab, out=leaf)
+    assert torch.equal(leaf.detach(), x)
+    # a tensor that a graph has saved, written without gradients: autograd notices
+    leaf = x.clone().requires_grad_()
+    saved = x.clone()
+    product = (leaf * saved).sum()
+    with torch.no_grad():
+        assert not G.gvr_rope_rotate(leaf, pos, tab).requires_grad
+        assert G.gvr_rope_rotate(saved, pos, tab, out=saved) is saved
+    with pytest.raises(RuntimeError):
+        product.backward()
+    with torch.inference_mode():
+        y = x.clone()
+        assert torch.equal(G.gvr_rope_rotate(y, pos, tab, out=y), G.gvr_rope_rotate(x, pos, tab))
+    assert not G.prepare_gvr_rope_rotate(leaf, pos, tab)().requires_grad
