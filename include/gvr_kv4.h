@@ -91,7 +91,7 @@ gvr_status gvr_kv4_read(const gvr_kv4_cache* cache, const gvr_heads* k, const gv
  *
  * Numerics: the stored keys enter the matrix cores as they are, the queries as
  * sums of two 8-bit numbers (three for float16) with a common scale per 32
- * elements: exact down to 2^-14 (2^-18) of the block's largest magnitude and
+ * elements: exact down to 2^-13 (2^-14) of the block's largest magnitude and
  * off by at most 2^-21 (2^-25) of it below. A score sums in float32 and is off
  * by about 2^-16 of scale * sum |q k|. The softmax's maximum and sum are
  * float32; the weights, relative to the largest, and the stored values (exact;

@@ -12,7 +12,7 @@
 //     scale byte is the instruction's block scale. The queries are its 8-bit
 //     operand: each is the sum of two E4M3 numbers (three for float16) with
 //     power-of-two scales 2^-4 apart, which holds a bfloat16 exactly down to
-//     2^-14 of its block's largest magnitude (an error of at most 2^-21 of it
+//     2^-13 of its block's largest magnitude (an error of at most 2^-21 of it
 //     below). Against unpacking K for the 16-bit instruction this costs the
 //     same matrix time and 32 vector instructions a step less;
 //   - the scores that come out sit in the lane that feeds them, as weights, to
