@@ -70,8 +70,8 @@ gvr_status gvr_rope_table(int64_t n, const gvr_rope_params* params, double gain,
  * (16-byte aligned rows with rot and D - rot multiples of 16 take the wide
  * loads).
  * Errors: GVR_ERR_INVALID_ARG (a NULL or misaligned pointer, T < 0, H < 0, a
- * bad D, rot, dtype, flag or positions count), GVR_ERR_TOO_LONG (T or H
- * above 2^31 - 16), GVR_ERR_HIP. T == 0 or H == 0 is a no-op. */
+ * bad D, rot, dtype, flag or positions count), GVR_ERR_TOO_LONG (T above
+ * 2^31 - 16 or H above 2^20), GVR_ERR_HIP. T == 0 or H == 0 is a no-op. */
 gvr_status gvr_rope_rotate(const gvr_heads* x, const gvr_heads* out, int32_t dtype, int64_t T, int32_t H, int32_t D,
                            const int32_t* positions, const gvr_rope_cs* cs, void* stream);
 

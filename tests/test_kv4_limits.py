@@ -45,3 +45,12 @@ def test_more_threads_than_a_launch_holds(K):
     assert attention(K, selection=64, K=5, sequences=1, T=1 << 23, max_q=1 << 23, heads=8, q_heads=8, **far) == -5
     assert attention(K, sequences=1 << 14, T=1 << 19, max_q=1 << 19, **far) == -5
     assert attention(K, sequences=1 << 13, T=1 << 19, max_q=1 << 19, D=256, **far) == -5
+
+
+def test_heads_of_a_rotation(K):
+    """2^20 heads at most, as gvr_rotary.h says."""
+    xs, cs = K._Heads(256, 64, 64), K._RopeCs(64, 100, 64, 0)
+    for H, want in ((1 << 20, 0), ((1 << 20) + 1, -5)):
+        assert K.lib().gvr_rope_rotate(ctypes.byref(xs), ctypes.byref(xs), 0, 0, H, 64, vp(64), ctypes.byref(cs), None) == want
+    header = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "gvr_rotary.h")
+    assert "H above 2^20" in open(header).read()
