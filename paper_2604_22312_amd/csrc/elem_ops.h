@@ -14,7 +14,9 @@
 namespace gvr_elem {
 
 typedef float f8 __attribute__((ext_vector_type(8)));
-template <class E> struct Vec8 { typedef E t __attribute__((ext_vector_type(8))); };
+// (eight float32 would ask for 32-byte alignment; rows promise 16)
+template <class E> struct Vec8 { typedef E t __attribute__((ext_vector_type(8), aligned(16))); };
+static_assert(alignof(Vec8<float>::t) == 16 && alignof(Vec8<__bf16>::t) == 16, "what 16-byte aligned rows hold");
 
 // Eight elements at p; wide: p is 16-byte aligned.
 template <bool WIDE, class E>
