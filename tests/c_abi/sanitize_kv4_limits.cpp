@@ -57,6 +57,9 @@ int main() {
         const int64_t rows = gvr_rot::table_rows(n);
         CHECK((n + rows - 1) / rows * 256 <= kMaxThreads && rows * 256 < (1 << 24));
     }
+    // sizes at which the GPU tests count on two heads a thread
+    CHECK(gvr_rot::plan_items(8193, 33, 6, 2).heads_each == 2 && gvr_rot::plan_items(701, 33, 64, 2).heads_each == 2);
+    CHECK(gvr_rot::plan_items(4097, 33, 8, 2).heads_each == 2 && gvr_rot::plan_items(4097, 33, 6, 2).heads_each == 1);
     std::puts("ok");
     return 0;
 }

@@ -35,6 +35,69 @@ def test_table_of_more_than_2_30_positions(G):
     assert np.abs(got - ref).max() <= 2.0 ** -24 + 2.0 ** -21
 
 
+def heads_each(T, H, per_head):
+    """Heads that a thread serves (plan_items of csrc/rotary_plan.h)."""
+    return 2 if H > 1 and T * H * per_head // 2 >= 256 * 2048 else 1
+
+
+@pytest.mark.parametrize("inv", [False, True])
+@pytest.mark.parametrize("dtype,inter,aligned,T", [("bf16", False, True, 8193), ("bf16", True, True, 8193),
+                                                   ("f32", False, True, 8193), ("f16", True, True, 8193),
+                                                   ("bf16", False, False, 701), ("f32", True, False, 701)])
+def test_two_heads_of_a_thread_and_a_last_one(G, dtype, inter, aligned, T, inv):
+    """An odd number of heads where threads serve two: the last head is there, and what lies beside the heads is not
+    touched. Wide and element-wise kernel."""
+    H, D, rot, P = 33, 96, 64, 200
+    assert heads_each(T, H, D // 16 if aligned else rot // 2 + D - rot) == 2
+    rng = np.random.default_rng(T + inter)
+    tab = O.rope_table(P, rot, 1.1).astype(np.float32)
+    pos = rng.integers(0, P, T).astype(np.int32)
+    at = 8 if aligned else 3
+    wide = torch.randn((T, H + 2, D + 16), generator=torch.Generator(device=DEV).manual_seed(T), device=DEV).to(TORCH[dtype])
+    x, out = wide[:, 1:1 + H, at:at + D], torch.full_like(wide, 9.0)
+    y = out[:, 1:1 + H, at:at + D]
+    note("rotate two heads a thread: %s inter=%s aligned=%s T=%d inv=%s" % (dtype, inter, aligned, T, inv))
+    G.gvr_rope_rotate(x, torch.from_numpy(pos).to(DEV), torch.from_numpy(tab).to(DEV), inter, inv, out=y)
+    want = O.rotate(x.cpu().float().numpy(), pos, tab, inter, inv)
+    assert torch.equal(y.cpu(), torch.from_numpy(want).to(TORCH[dtype]))
+    y.fill_(9.0)
+    assert (out == 9.0).all()
+
+
+@pytest.mark.parametrize("dtype,rot,inter,aligned", [("bf16", 0, False, True), ("bf16", 64, False, True), ("f32", 32, False, True),
+                                                     ("f16", 64, True, True), ("f32", 24, True, False), ("bf16", 64, False, False)])
+def test_append_and_read_two_heads_of_a_thread(G, dtype, rot, inter, aligned):
+    """As above for the cache: records equal the oracle's, other records stay, and tokens read back stand beside
+    untouched heads."""
+    T, H, D, P, page = 4097, 33, 64, 200, 64
+    assert heads_each(T, H, D // 8) == 2
+    rng = np.random.default_rng(rot + aligned)
+    tab = O.rope_table(P, rot, 1.1).astype(np.float32) if rot else None
+    pos = rng.integers(0, P, T).astype(np.int32)
+    at = 8 if aligned else 3
+    wide = torch.randn((2, T, H + 1, D + 16), generator=torch.Generator(device=DEV).manual_seed(rot), device=DEV).to(TORCH[dtype])
+    k, v = wide[0, :, :H, at:at + D], wide[1, :, 1:, at:at + D]
+    pages = (T + page - 1) // page + 1
+    slots = rng.permutation(pages * page)[:T].astype(np.int64)
+    cache = torch.full((pages, page, G.gvr_kv4_record_bytes(H, D)), 77, dtype=torch.uint8, device=DEV)
+    kw = dict(table=torch.from_numpy(tab).to(DEV), positions=torch.from_numpy(pos).to(DEV), interleaved=inter) if rot else {}
+    note("append two heads a thread: %s rot=%d inter=%s aligned=%s" % (dtype, rot, inter, aligned))
+    G.gvr_kv4_append(k, v, torch.from_numpy(slots).to(DEV), cache, **kw)
+    k32 = k.cpu().float().numpy()
+    rec = O.record(O.rotate(k32, pos, tab, inter) if rot else k32, v.cpu().float().numpy())
+    want = np.full((pages * page, rec.shape[1]), 77, np.uint8)
+    want[slots] = rec
+    assert np.array_equal(cache.cpu().numpy().reshape(want.shape), want)
+    back = torch.full_like(wide, 9.0)
+    bk, bv = back[0, :, :H, at:at + D], back[1, :, 1:, at:at + D]
+    G.gvr_kv4_read(cache, torch.from_numpy(slots).to(DEV), H, D, dtype=TORCH[dtype], k=bk, v=bv)
+    ek, ev = O.values(rec, H, D)
+    assert np.array_equal(f64(bk), ek) and np.array_equal(f64(bv), ev)
+    bk.fill_(9.0)
+    bv.fill_(9.0)
+    assert (back == 9.0).all()
+
+
 # ---- gradients through autograd
 
 def rotary(rng, T=9, H=3, D=48, rot=40, dtype="f32", gain=1.2, P=100):
