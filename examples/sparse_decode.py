@@ -38,6 +38,7 @@ class SparseLayer:
         self.blocks = torch.randperm(requests * pages, device=device).to(torch.int32).view(requests, pages)
         self.table = gvr.gvr_rope_table(longest, dict(d_rope=head_dim), gain=1.0, device=device)
         self.length = torch.zeros(requests, dtype=torch.int32, device=device)
+        self.longest, self.tokens = longest, 0   # (of each request, known without asking the device)
         # the indexer's keys: FP8 bytes and a scale per token
         self.index_k = torch.zeros((requests, longest, index_dim), dtype=torch.uint8, device=device)
         self.index_scale = torch.ones((requests, longest), device=device)
@@ -46,6 +47,9 @@ class SparseLayer:
 
     def _store(self, k, v, index_k, new):
         """Append `new` tokens of every request; their positions (int32 [R * new])."""
+        if self.tokens + new > self.longest:
+            raise ValueError("%d tokens a request, of at most %d" % (self.tokens + new, self.longest))
+        self.tokens += new
         pos = self.length.view(-1, 1) + torch.arange(new, dtype=torch.int32, device=self.dev)
         slots = torch.gather(self.blocks, 1, (pos // self.page).long()).long() * self.page + pos % self.page
         pos = pos.view(-1)
