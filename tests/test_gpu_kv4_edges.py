@@ -6,7 +6,7 @@ import torch
 
 from oracle import kv4 as O
 from tests.gpu_cases import note
-from tests.kv4_cases import DEV, TORCH, UNIT, Sequences, f64
+from tests.kv4_cases import DEV, TORCH, UNIT, Sequences, check_attention, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -150,3 +150,55 @@ def test_max_q_of_any_size(G, max_q):
     out = G.gvr_kv4_attention(q, cache, table, lens, 1, q_start=start, max_q=max_q, out=torch.full_like(q, 3.0))
     served = min(max_q, 9)
     assert (out[served:] == 3).all() and torch.equal(out[:served], want[:served])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,heads,group", [(64, 2, 4), (128, 1, 8), (128, 1, 40), (256, 2, 2)])
+def test_selection_over_a_prompt(G, D, heads, group, dtype):
+    """A list for every query token of a prompt: whole ones, short ones (-1 behind), and the first tokens' few."""
+    rng = np.random.default_rng(66)
+    ctx, nq, K = [300, 70, 0], 70, 48
+    seqs = Sequences(rng, ctx, 16, heads, D)
+    cache, table, lens = seqs.on_gpu()
+    sel = np.full((len(ctx) * nq, K), -1, np.int32)
+    for b, c in enumerate(ctx):
+        for i in range(nq):
+            see = max(0, c - nq + 1 + i)
+            pick = np.sort(rng.permutation(see)[:K - 20 * (i % 3 == 2)])
+            sel[b * nq + i, :len(pick)] = pick
+    q = torch.from_numpy(rng.standard_normal((len(ctx) * nq, heads * group, D))).to(TORCH[dtype]).to(DEV)
+    note("selection over a prompt: %s D=%d heads=%d group=%d" % (dtype, D, heads, group))
+    lse = torch.empty((q.shape[0], q.shape[1]), device=DEV)
+    out = G.gvr_kv4_attention(q, cache, table, lens, heads, selection=torch.from_numpy(sel).to(DEV), lse=lse)
+    check_attention(out, lse, q, seqs, [nq * b for b in range(len(ctx) + 1)], D ** -0.5, selection=sel, dtype=dtype,
+                    what="selection over a prompt")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,group,nq", [(64, 2, 4), (64, 5, 7), (128, 16, 3), (128, 4, 40), (256, 2, 70), (64, 1, 140)])
+def test_rows_beside_nan_blocks_are_right(G, dtype, D, group, nq):
+    """Value and key blocks that are NaN, in tokens that only the later queries see: the earlier rows equal the oracle's
+    within their roundings, split or not."""
+    rng = np.random.default_rng(67)
+    n, split = 300, nq // 2
+    first = n - nq + split
+    k, v = rng.standard_normal((n, 1, D)), rng.standard_normal((n, 1, D))
+    v[first:, 0, 40] = np.nan
+    k[first + 1:, 0, 3] = np.inf
+    cache, table, lens, kk, vv = held(k, v)
+    q = torch.from_numpy(rng.standard_normal((nq, group, D))).to(TORCH[dtype]).to(DEV)
+    u, scale = UNIT[dtype], D ** -0.5
+    for ws in (torch.empty(0, dtype=torch.uint8, device=DEV), None):
+        note("rows beside NaN: %s D=%d group %d nq %d %s" % (dtype, D, group, nq, "split" if ws is None else "whole"))
+        out = f64(G.gvr_kv4_attention(q, cache, table, lens, 1, workspace=ws))
+        for i in range(nq):
+            t = n - nq + i + 1
+            if i >= split:
+                seen = out[i] if i > split else out[i][:, 32:64]     # a NaN key: everything; a NaN value: its block
+                assert np.isnan(seen).all() and (i > split or np.isfinite(out[i][:, :32]).all())
+                continue
+            ref, _, mag = O.attention(f64(q)[i], kk[:t], vv[:t], scale)
+            qk = (np.abs(kk[:t, 0]) @ np.abs(f64(q)[i]).T).max()
+            eps = ((D + 8) * scale * qk + t + 64) * 2.0 ** -24
+            tol = (u + 2 * eps) * (1 + u) * mag + u * np.abs(ref) + t * 2.0 ** -40 * np.abs(vv[:t]).max() + 2.0 ** -25
+            assert (np.abs(out[i] - ref) <= tol).all(), "row %d" % i
