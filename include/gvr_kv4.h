@@ -77,7 +77,9 @@ gvr_status gvr_kv4_read(const gvr_kv4_cache* cache, const gvr_heads* k, const gv
  * is place t % page_size of page block_table[b][t / page_size]; a page number
  * outside [0, pages) makes its tokens invisible. The sequence's query tokens
  * are rows q_start[b] .. q_start[b+1]-1 of q (n_q of them, at most max_q are
- * served; q_start NULL: T / sequences each). The queries are the last tokens
+ * served, and rows that are not served are not written; the launch is planned
+ * for max_q rows of every sequence, so it should be no more than their most;
+ * q_start NULL: T / sequences each). The queries are the last tokens
  * of the context: with `causal`, query i sees t <= ctx_len[b] - n_q + i, else
  * every t < ctx_len[b]. With `selection` [T][K] int32, query row r attends
  * only to the tokens that its list names and the rule above allows (entries
@@ -116,7 +118,7 @@ typedef struct gvr_kv4_attention_args {
     int64_t T;
     int64_t table_width;         /* pages per sequence */
     int32_t sequences;
-    int32_t max_q;               /* most query tokens of a sequence (with q_start) */
+    int32_t max_q;               /* most query tokens of a sequence (with q_start; else not read) */
     int32_t q_heads;             /* a multiple of kv_heads, at most 128 * kv_heads */
     int32_t K;                   /* selection entries per row */
     int32_t dtype;               /* GVR_BF16 or GVR_F16 */

@@ -38,18 +38,24 @@
 // every step: 43 us against 59 with the host's). Units that read the same records go to one XCD.
 //
 // What bounds it, measured (MI355X; a plain read of as many bytes in brackets):
-//   32 x 32K tokens, 8 KV heads of 128, 4 rows each: 208 us = 5.5 TB/s (166 us);
+//   32 x 32K tokens, 8 KV heads of 128, 4 rows each: 210 us = 5.4 TB/s (166 us);
 //     memory: the same loads with nothing computed take 205 us, because a head's
 //     64 bytes of codes per record are half a line, and its eight waves do not
 //     ask for both halves at once;
-//   1 x 512K tokens, 8 rows: 116 us (83 us): the same, and the join of 256 parts;
+//   1 x 512K tokens, 8 rows: 117 us (83 us): the same, and the join of 256 parts;
 //   128 rows of 2048 selected tokens: 61 us (41 us for what the rows select
 //     one by one, 24 for what two draft rows have in common): gathers of 1 KB;
-//   48 x 3 rows over 0 .. 16K tokens, 2 KV heads of 64, float16: 34 us (7.5 us):
+//   48 x 3 rows over 0 .. 16K tokens, 2 KV heads of 64, float16: 35 us (7.5 us):
 //     12 us before the first record (lengths, splits, pages), 6 of join, and steps at
 //     2.6 TB/s, which two row tiles of dependent products and exponentials set;
-//   1 x 1K tokens: 12.6 us: latency, of two launches and in the first of them
+//   1 x 1K tokens: 12.5 us: latency, of two launches and in the first of them
 //     length -> page -> record -> join.
+// All of it where the table of pages is about as wide as the contexts are long:
+// the host plans by the table's width (64 heads over one request of 32K tokens in
+// a table for as many 20 us, for 512K, with work for 16 workgroups, 95; a chunk of 512
+// tokens at 8K, 32 heads, in a table for 8K 117 us, for 128K 311; 32 requests of 8K, which the
+// kernel balances, 62 and 60). And a selection costs what its K entries do, also
+// where they are -1 (64 rows of 300 tokens: K = 320 12 us, 2048 34).
 // More than 128 rows of a KV head: see "many query rows" below.
 
 #include <hip/hip_runtime.h>
@@ -864,9 +870,13 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
 // scores' registers name them), unpacked once for all the rows. Two buffers: a
 // tile is unpacked into one while the other is used, and the records of the
 // tile after it are on their way in registers.
-// 4096 rows of 32 heads over 32K tokens, 8 KV heads of 128: 1.93 ms, 1.07
-// PFLOP/s, against 3.83 ms with the few-rows kernel. Bound by the vector unit
-// beside the matrix cores: exponentials, packing and the unpacking of V. For 128
+// 4096 rows of 32 heads over 32K tokens, 8 KV heads of 128: 1.95 to 2.02 ms, 1.02
+// to 1.06 PFLOP/s (calls back to back, at lower clocks: 2.2 to 2.4 ms), against
+// 3.83 ms with the few-rows kernel. Bound by the vector unit beside the matrix
+// cores: exponentials, packing and the unpacking of V. Float16, with three terms
+// of the queries, is slower: 2048 rows over 16K tokens 665 us against 541 (D = 64:
+// 386; D = 256, 1024 rows of 16 heads: 563), and at D = 128 and 256 its registers
+// spill (12 and 28 bytes a lane). At D = 256 a SIMD has one wave. For 128
 // rows and fewer the few-rows kernel is ahead (32 x 8K tokens: 64 rows 139 us
 // against 234, 128 rows 256 against 274, 192 rows 398 against 348): half of this
 // one's rows are then empty.

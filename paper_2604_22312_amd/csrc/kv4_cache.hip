@@ -10,8 +10,9 @@
 // is read once and 4.25 bits of each written (16384 tokens of 8 heads of 128
 // with rotation, appended and read back from HBM: 43 us = 4.2 TB/s; the append
 // alone, what it reads still in the caches, 19, the reading 15); one token: 4 us
-// each, the launch. Unaligned rows load element by element (append 18 us
-// against 43).
+// each, the launch and four or five loads one after the other (slot, position,
+// table row, key, in the half layout its partner). Unaligned rows load element by
+// element (that append: 43 us against 18).
 
 #include <hip/hip_runtime.h>
 

@@ -362,10 +362,14 @@ def gvr_kv4_attention(q, cache, block_table, ctx_len, kv_heads, selection=None, 
     block_table (int32 [sequences][pages]) and ctx_len (int32 [sequences])
     describe the sequences; each has T / sequences query tokens, or rows
     q_start[b] .. q_start[b+1]-1 (int32 [sequences + 1], at most ``max_q``
-    each). ``selection`` (int32 [T][K], -1 padded: ``gvr_topk``'s result)
+    each; the others' rows of ``out`` and ``lse`` are not written). With
+    ``q_start``, give ``max_q``: the launch is planned for that many rows of
+    every sequence, and for all T of them if it is None (48 sequences of 3 rows:
+    340 us instead of 38). ``selection`` (int32 [T][K], -1 padded: ``gvr_topk``'s result)
     restricts each row to the listed tokens. ``causal``: the queries are the
     last tokens of the context. ``lse`` (float32 [T][q_heads]) receives the
     log of the softmax's sum. ``workspace``: device memory for split contexts
-    (``gvr_kv4_attention_workspace`` bytes; allocated for the call if None)."""
+    (``gvr_kv4_attention_workspace`` bytes; allocated for the call if None).
+    The cache is a serving store: no gradient is recorded."""
     return prepare_gvr_kv4_attention(q, cache, block_table, ctx_len, kv_heads, selection, q_start, max_q, causal, scale,
                                      out, lse, workspace, stream)()
