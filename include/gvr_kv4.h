@@ -95,16 +95,16 @@ gvr_status gvr_kv4_read(const gvr_kv4_cache* cache, const gvr_heads* k, const gv
  * sums of two 8-bit numbers (three for float16) with a common scale per 32
  * elements: exact down to 2^-13 (2^-14) of the block's largest magnitude and
  * off by at most 2^-21 (2^-25) of it below. A score sums in float32 and is off
- * by about 2^-16 of scale * sum |q k|. The softmax's maximum and sum are
- * float32; the weights, relative to the largest, and the stored values (exact;
- * with float16 queries they must be below 65520) enter the second product in
- * the queries' type (float16: a weight is off by at most 2^-40 of the largest
- * beside its rounding); it sums in float32, and the result is rounded once:
- * about 0.0017 relative error in bfloat16, of which 0.0016 is that last
- * rounding. Rounding
- * depends on how the context is split (the workspace below, and with several
- * sequences their lengths), never on timing: the same call gives the same
- * bits. */
+ * by about 2^-16 of scale * sum |q k|; in bfloat16 scale * (q . k) must stay
+ * below 2^30 in magnitude. The softmax's maximum and sum are float32; the
+ * weights, relative to the largest, and the stored values (exact; with float16
+ * queries they must be below 65520, and are rounded to multiples of 2^-24) enter
+ * the second product in the queries' type (float16: a weight is off by at most
+ * 2^-40 of the largest beside its rounding); it sums in float32, and the result
+ * is rounded once: about 0.0017 relative error in bfloat16, of which 0.0016 is
+ * that last rounding. Rounding depends on how the context is split (the
+ * workspace below, and with several sequences their lengths), never on timing:
+ * the same call gives the same bits. */
 typedef struct gvr_kv4_attention_args {
     const void* q;               /* [T][q_heads][head_dim], 16-byte aligned rows */
     int64_t q_token_stride;      /* elements, multiples of 8 */

@@ -202,3 +202,23 @@ def test_rows_beside_nan_blocks_are_right(G, dtype, D, group, nq):
             eps = ((D + 8) * scale * qk + t + 64) * 2.0 ** -24
             tol = (u + 2 * eps) * (1 + u) * mag + u * np.abs(ref) + t * 2.0 ** -40 * np.abs(vv[:t]).max() + 2.0 ** -25
             assert (np.abs(out[i] - ref) <= tol).all(), "row %d" % i
+
+
+@pytest.mark.parametrize("dtype", ["f16"])
+@pytest.mark.parametrize("D,nq", [(64, 1), (128, 20), (128, 70), (256, 1), (256, 70)])
+@pytest.mark.parametrize("scale", [1e6, -1e6, 3e28])
+def test_scores_past_2_31(G, dtype, D, nq, scale):
+    """One token takes all the weight where the scores pass 2^31, up to 1e34 (float16; bfloat16 is for less, as its
+    header says)."""
+    rng = np.random.default_rng(68)
+    k, v = one_ahead(900, D, 3.0, rng)
+    k[:, 0, 1] = 6.0
+    if scale < 0:
+        k = -k
+    cache, table, lens, _, vv = held(k, v)
+    q = torch.zeros((nq, 2, D), dtype=TORCH[dtype], device=DEV)
+    q[:, :, 0] = q[:, :, 1] = 60000.0
+    for ws in (torch.empty(0, dtype=torch.uint8, device=DEV), None):
+        note("scores past 2^31: %s D=%d nq=%d scale %g" % (dtype, D, nq, scale))
+        out = G.gvr_kv4_attention(q, cache, table, lens, 1, scale=scale, causal=False, workspace=ws)
+        assert np.array_equal(f64(out), np.broadcast_to(vv[7], out.shape))
