@@ -954,7 +954,8 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void many_rows_kernel(At
     // last token that this lane's row sees; that all rows of the wave see; tokens that concern the workgroup
     const int last = !live ? -1 : p.causal ? (int)(ctx - nq + qi) : ctx - 1;
     const int all_last = (int)max((int64_t)-1, p.causal ? ctx - nq + (first_row + 32 * wave) / p.group : (int64_t)ctx - 1);
-    const int wg_last = (int)max((int64_t)-1, p.causal ? ctx - nq + first_row / p.group : (int64_t)ctx - 1);
+    // (no row sees less than another where it is not causal)
+    const int wg_last = p.causal ? (int)max((int64_t)-1, ctx - nq + first_row / p.group) : 0x7FFFFFFF;
     const int wave_last_q = min((first_row + 32 * wave + 31) / p.group, shown - 1);
     const int wave_last = (first_row + 32 * wave) / p.group >= shown ? -1
                           : p.causal ? (int)max((int64_t)-1, ctx - nq + wave_last_q) : ctx - 1;   // that any row of the wave sees

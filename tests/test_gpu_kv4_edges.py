@@ -222,3 +222,29 @@ def test_scores_past_2_31(G, dtype, D, nq, scale):
         note("scores past 2^31: %s D=%d nq=%d scale %g" % (dtype, D, nq, scale))
         out = G.gvr_kv4_attention(q, cache, table, lens, 1, scale=scale, causal=False, workspace=ws)
         assert np.array_equal(f64(out), np.broadcast_to(vv[7], out.shape))
+
+
+@pytest.mark.parametrize("dtype,huge", [("f16", 60000.0), ("bf16", 3.3e38)])
+@pytest.mark.parametrize("D,group,nq", [(64, 4, 1), (128, 16, 3), (128, 4, 40), (256, 2, 70), (64, 1, 140)])
+def test_visible_infinities_stay_in_their_dimension(G, dtype, huge, D, group, nq):
+    """Values that the 16-bit type cannot hold, in tokens that every query sees (not causal; the first and the last): the
+    other dimensions are right, those of the same block of 32 among them."""
+    rng = np.random.default_rng(70)
+    n = 300
+    k, v = rng.standard_normal((n, 1, D)), rng.standard_normal((n, 1, D))
+    v[[3, n - 1], 0, 32:64] = 0.0               # (beside the large value every other is less than half a step)
+    v[[3, n - 1], 0, 40] = huge
+    cache, table, lens, kk, vv = held(k, v)
+    q = torch.from_numpy(rng.standard_normal((nq, group, D))).to(TORCH[dtype]).to(DEV)
+    u, scale = UNIT[dtype], D ** -0.5
+    rest = np.arange(D) != 40
+    for ws in (torch.empty(0, dtype=torch.uint8, device=DEV), None):
+        note("visible infinities: %s D=%d group %d nq %d %s" % (dtype, D, group, nq, "split" if ws is None else "whole"))
+        out = f64(G.gvr_kv4_attention(q, cache, table, lens, 1, causal=False, workspace=ws))
+        assert not np.isfinite(out[..., 40]).any()
+        for i in range(nq):
+            ref, _, mag = O.attention(f64(q)[i], kk, vv, scale)
+            qk = (np.abs(kk[:, 0]) @ np.abs(f64(q)[i]).T).max()
+            eps = ((D + 8) * scale * qk + n + 64) * 2.0 ** -24
+            tol = (u + 2 * eps) * (1 + u) * mag + u * np.abs(ref) + n * 2.0 ** -40 * np.abs(vv[:, 0, rest]).max() + 2.0 ** -25
+            assert (np.abs(out[i] - ref) <= tol)[:, rest].all(), "row %d" % i
