@@ -167,8 +167,8 @@ DEV float max_rows(float x) {
 // whole result, and would be lost). So they are 2^15 times as large there, which
 // moves that limit to 2^-40, and sum and O are scaled back at the end. Base is
 // the maximum itself, so that the largest is 2^15 whatever the scores' size: one
-// more subtraction a weight (2048 rows of 32 heads over 16K tokens, D = 64: 386 us
-// against 374, D = 128: 670, 651; 32 x 8K tokens 60.7, 60.0).
+// more subtraction a weight (2048 rows of 32 heads over 16K tokens, D = 64: 385 us
+// against 374, D = 128: 655 to 695 against 640 to 660; 32 x 8K tokens 60.6, 60.0).
 constexpr float kUp = 15.f, kDown = 1.f / 32768;
 template <class E>
 DEV float base_of(float m, float scale2) {
@@ -874,8 +874,8 @@ __global__ __launch_bounds__(kThreads, D == 64 && MT == 1 && __is_same(E, __bf16
 // to 1.06 PFLOP/s (calls back to back, at lower clocks: 2.2 to 2.4 ms), against
 // 3.83 ms with the few-rows kernel. Bound by the vector unit beside the matrix
 // cores: exponentials, packing and the unpacking of V. Float16, with three terms
-// of the queries, is slower: 2048 rows over 16K tokens 665 us against 541 (D = 64:
-// 386; D = 256, 1024 rows of 16 heads: 563), and at D = 128 and 256 its registers
+// of the queries, is slower: 2048 rows over 16K tokens 655 to 695 us against 540 (D = 64:
+// 385; D = 256, 1024 rows of 16 heads: 557), and at D = 128 and 256 its registers
 // spill (12 and 28 bytes a lane). At D = 256 a SIMD has one wave. For 128
 // rows and fewer the few-rows kernel is ahead (32 x 8K tokens: 64 rows 139 us
 // against 234, 128 rows 256 against 274, 192 rows 398 against 348): half of this
