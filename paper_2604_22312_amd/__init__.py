@@ -5,7 +5,9 @@ Thin Python binding over the C ABI of ``include/gvr_topk.h`` (library
 only validates tensors and marshals pointers; every step of the Top-K runs in
 the HIP kernels of ``csrc/gvr_topk.hip``, ``csrc/rope_prior.hip`` and
 ``csrc/indexer.hip`` (rotary positions and the 4-bit cache:
-``csrc/rotary.hip``, ``csrc/kv4_cache.hip``, ``csrc/kv4_attention.hip``). There is no CPU fallback: if the
+``csrc/rotary.hip``, ``csrc/kv4_cache.hip``, ``csrc/kv4_attention.hip``; pages
+and 8-bit matrices: ``csrc/pages.hip``, ``csrc/fp8_quantize.hip``,
+``csrc/fp8_matmul.hip``). There is no CPU fallback: if the
 library is missing, importing the functions raises.
 
 Functions mirror the C entry points:
@@ -34,6 +36,12 @@ Functions mirror the C entry points:
   ``gvr_kv4_attention`` -- the paged 4-bit key / value cache: tokens in (keys
   rotated on the way) and out, and attention over all of a context or over
   the tokens a Top-K selected (``include/gvr_kv4.h``)
+* ``new_page_pool`` / ``gvr_page_step`` -- block tables, slots, positions and row
+  starts from the tokens that requests keep and bring (``include/gvr_pages.h``)
+* ``gvr_fp8_quantize`` / ``gvr_fp8_quantize_matrix`` / ``gvr_fp8_matmul`` /
+  ``gvr_fp8_linear`` -- E4M3 codes with a scale per 128 elements: of heads (rotated,
+  into the indexer's key cache) and matrices, their products, and a linear layer of
+  them with its gradients (``include/gvr_fp8.h``)
 """
 from .binding import (  # noqa: F401
     GVR_MAX_CANDIDATES,
@@ -67,6 +75,17 @@ from .binding import (  # noqa: F401
     status_string,
     version,
 )
+from .fp8 import (  # noqa: F401
+    Fp8Matrix,
+    gvr_fp8_linear,
+    gvr_fp8_matmul,
+    gvr_fp8_matmul_workspace,
+    gvr_fp8_quantize,
+    gvr_fp8_quantize_matrix,
+    prepare_gvr_fp8_matmul,
+    prepare_gvr_fp8_quantize,
+    prepare_gvr_fp8_quantize_matrix,
+)
 from .kv4 import (  # noqa: F401
     PreparedOp,
     gvr_kv4_append,
@@ -81,4 +100,12 @@ from .kv4 import (  # noqa: F401
     prepare_gvr_kv4_attention,
     prepare_gvr_kv4_read,
     prepare_gvr_rope_rotate,
+)
+from .pages import (  # noqa: F401
+    PagePool,
+    PageStep,
+    gvr_page_step,
+    gvr_page_step_workspace,
+    new_page_pool,
+    prepare_gvr_page_step,
 )

@@ -10,7 +10,8 @@ from concurrent.futures import ThreadPoolExecutor
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SOURCES = [os.path.join(PKG, "csrc", f) for f in ("gvr_topk.hip", "rope_prior.hip", "indexer.hip", "read_floor.hip",
-                                                 "rotary.hip", "kv4_cache.hip", "kv4_attention.hip")]
+                                                 "rotary.hip", "kv4_cache.hip", "kv4_attention.hip",
+                                                 "pages.hip", "fp8_quantize.hip", "fp8_matmul.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libgvr_topk.so")
 ARCH = "gfx950"

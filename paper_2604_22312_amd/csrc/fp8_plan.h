@@ -1,0 +1,108 @@
+// fp8_plan.h -- argument checks and launch plans of the 8-bit matrices: making
+// them and multiplying them. Plain C++ with no HIP dependency, so the library
+// and a sanitizer build on the CPU compile the same code.
+#ifndef GVR_FP8_PLAN_H
+#define GVR_FP8_PLAN_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "gvr_fp8.h"
+#include "rotary_plan.h"
+
+namespace gvr_fp8 {
+
+using gvr_rot::kMaxCount;
+
+constexpr int kGroup = 128;       // elements that share a scale
+constexpr int kBlock = 256;       // threads of the quantising kernels
+constexpr int kMaxHead = 1 << 20; // elements of a head, and heads
+
+inline int64_t groups_of(int64_t n) { return (n + kGroup - 1) / kGroup; }
+
+// --- heads: 16 lanes take a block of 128 elements, eight each
+struct HeadsPlan {
+    int64_t tokens, blocks, rows;   // of a launch row (blockIdx.y), workgroups in x, launch rows
+};
+inline HeadsPlan plan_heads(int64_t T, int64_t lanes_per_token) {
+    HeadsPlan p;
+    p.tokens = kMaxCount / lanes_per_token;
+    if (p.tokens > T) p.tokens = T;
+    if (p.tokens < 1) p.tokens = 1;
+    p.blocks = (p.tokens * lanes_per_token + kBlock - 1) / kBlock;
+    p.rows = (T + p.tokens - 1) / p.tokens;
+    return p;
+}
+
+inline gvr_status check_heads(const gvr_heads* x, int dtype, int64_t T, int H, int D, const int32_t* positions,
+                              const gvr_rope_cs* cs, const gvr_fp8_heads* out, const int64_t* slots, int64_t rows,
+                              int flags) {
+    const int size = gvr_rot::dtype_size(dtype);
+    if (!x || !out || size == 0 || T < 0 || H < 0 || D < 1 || rows < 0 || (flags & ~GVR_FP8_POW2)) return GVR_ERR_INVALID_ARG;
+    if (T > kMaxCount || rows > kMaxCount || H > kMaxHead || D > kMaxHead) return GVR_ERR_TOO_LONG;
+    if (((uintptr_t)x->data & (size - 1)) || ((uintptr_t)out->scale & 3) || ((uintptr_t)slots & 7)) return GVR_ERR_INVALID_ARG;
+    if (cs) {
+        const gvr_status st = gvr_rot::check_cs(*cs, D, GVR_ROPE_INTERLEAVED);
+        if (st != GVR_OK) return st;
+        if (T > 0 && H > 0 && (!positions || ((uintptr_t)positions & 3))) return GVR_ERR_INVALID_ARG;
+    }
+    if (T == 0 || H == 0) return GVR_OK;
+    if (!x->data || !out->codes || !out->scale) return GVR_ERR_INVALID_ARG;
+    if (!slots && rows < T) return GVR_ERR_INVALID_ARG;
+    const int64_t lanes = (int64_t)H * groups_of(D) * 16;
+    if (lanes > kMaxCount || plan_heads(T, lanes).rows > gvr_rot::kMaxRows) return GVR_ERR_TOO_LONG;
+    return GVR_OK;
+}
+
+// --- matrices: a workgroup takes 128 x 128 elements
+inline gvr_status check_matrix(const gvr_fp8_matrix& m, int rows_per_scale, bool need) {
+    if (m.reserved != 0 || m.rows_per_scale != rows_per_scale) return GVR_ERR_INVALID_ARG;
+    if (need && (!m.codes || !m.scale)) return GVR_ERR_INVALID_ARG;
+    if ((uintptr_t)m.scale & 3) return GVR_ERR_INVALID_ARG;
+    return GVR_OK;
+}
+inline gvr_status check_quantize_matrix(const void* x, int dtype, int64_t R, int64_t C, const gvr_fp8_matrix* straight,
+                                        const gvr_fp8_matrix* transposed, int flags) {
+    const int size = gvr_rot::dtype_size(dtype);
+    if (size == 0 || R < 0 || C < 0 || (flags & ~(GVR_FP8_POW2 | GVR_FP8_SQUARE))) return GVR_ERR_INVALID_ARG;
+    const bool need = R > 0 && C > 0;
+    for (const gvr_fp8_matrix* m : {straight, transposed})
+        if (m) {
+            const gvr_status st = check_matrix(*m, flags & GVR_FP8_SQUARE ? kGroup : 1, need);
+            if (st != GVR_OK) return st;
+        }
+    if (R > kMaxCount || C > kMaxCount) return GVR_ERR_TOO_LONG;
+    if ((uintptr_t)x & (size - 1)) return GVR_ERR_INVALID_ARG;
+    if (!need || (!straight && !transposed)) return GVR_OK;
+    if (!x) return GVR_ERR_INVALID_ARG;
+    if (groups_of(R) * groups_of(C) >= (1 << 24)) return GVR_ERR_TOO_LONG;   // (a launch has fewer than 2^32 threads)
+    return GVR_OK;
+}
+
+// --- products
+inline gvr_status check_matmul(const gvr_fp8_matrix* a, const gvr_fp8_matrix* b, int64_t M, int64_t N, int64_t K,
+                               bool pointers) {
+    if (!a || !b || M < 0 || N < 0 || K < 0 || a->rows_per_scale != 1 || !(b->rows_per_scale == 1 || b->rows_per_scale == kGroup))
+        return GVR_ERR_INVALID_ARG;
+    const bool need = pointers && M > 0 && N > 0 && K > 0;
+    const gvr_status sa = check_matrix(*a, 1, need), sb = check_matrix(*b, b->rows_per_scale, need);
+    if (sa != GVR_OK || sb != GVR_OK) return GVR_ERR_INVALID_ARG;
+    if (M > kMaxCount || N > kMaxCount || K > kMaxCount) return GVR_ERR_TOO_LONG;
+    return GVR_OK;
+}
+
+constexpr int kTileM = 64, kTileN = 64, kThreads = 256;
+
+struct MatmulPlan {
+    int64_t tiles_m, tiles_n, workgroups;
+};
+inline gvr_status plan_matmul(int64_t M, int64_t N, MatmulPlan* p) {
+    p->tiles_m = (M + kTileM - 1) / kTileM;
+    p->tiles_n = (N + kTileN - 1) / kTileN;
+    p->workgroups = p->tiles_m * p->tiles_n;   // (each at most 2^25)
+    return p->workgroups * kThreads > 0xFFFFFFFFll ? GVR_ERR_TOO_LONG : GVR_OK;
+}
+
+}  // namespace gvr_fp8
+
+#endif  // GVR_FP8_PLAN_H
