@@ -92,15 +92,38 @@ inline gvr_status check_matmul(const gvr_fp8_matrix* a, const gvr_fp8_matrix* b,
 }
 
 constexpr int kTileM = 64, kTileN = 64, kThreads = 256;
+enum Shape { kAnyShape, kLarge, kSquare };
 
 struct MatmulPlan {
-    int64_t tiles_m, tiles_n, workgroups;
+    Shape shape;
+    int tile_m, tile_n, threads;
+    int64_t tiles_m, tiles_n, splits, steps_each, band, workgroups;
+    size_t workspace;   // bytes of the splits' parts
 };
-inline gvr_status plan_matmul(int64_t M, int64_t N, MatmulPlan* p) {
-    p->tiles_m = (M + kTileM - 1) / kTileM;
-    p->tiles_n = (N + kTileN - 1) / kTileN;
-    p->workgroups = p->tiles_m * p->tiles_n;   // (each at most 2^25)
-    return p->workgroups * kThreads > 0xFFFFFFFFll ? GVR_ERR_TOO_LONG : GVR_OK;
+
+// Rows that 16-byte loads can serve and that 32-bit offsets reach over a tile of
+// `rows` of them.
+inline bool tile_rows(const gvr_fp8_matrix& m, int rows, int64_t K) {
+    return ((uintptr_t)m.codes & 15) == 0 && m.row_stride % 16 == 0 && m.row_stride >= 0 &&
+           m.row_stride * rows + K < kMaxCount && m.scale_row_stride >= 0 && m.scale_block_stride >= 0 &&
+           m.scale_row_stride < (1 << 20) && m.scale_block_stride < (1 << 28) &&
+           (m.scale_row_stride * rows + m.scale_block_stride * groups_of(K)) * 4 < kMaxCount;
+}
+
+inline gvr_status plan_matmul(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, int64_t M, int64_t N, int64_t K, bool wide,
+                              size_t ws_bytes, MatmulPlan* p) {
+    const bool tiles = tile_rows(a, 256, K) && tile_rows(b, 256, K);
+    p->shape = !tiles ? kAnyShape : !wide && M * N >= (int64_t)256 * 256 * 128 ? kLarge : kSquare;
+    p->tile_m = p->tile_n = p->shape == kLarge ? 256 : p->shape == kSquare ? 128 : 64;
+    p->threads = p->shape == kLarge ? 512 : 256;
+    p->tiles_m = (M + p->tile_m - 1) / p->tile_m;
+    p->tiles_n = (N + p->tile_n - 1) / p->tile_n;   // (each at most 2^25)
+    p->splits = 1;
+    p->steps_each = groups_of(K);
+    p->band = 8;
+    p->workspace = 0;
+    p->workgroups = p->tiles_m * p->tiles_n * p->splits;
+    return p->workgroups * p->threads > 0xFFFFFFFFll ? GVR_ERR_TOO_LONG : GVR_OK;
 }
 
 }  // namespace gvr_fp8
