@@ -165,6 +165,18 @@ DEV void drain() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
 }
 
+template <int V>
+struct Int {
+    constexpr operator int() const { return V; }
+};
+template <int N, int I = 0, class F>
+DEV void each(F& f) {   // f(0) .. f(N - 1), known when compiled
+    if constexpr (I < N) {
+        f(Int<I>());
+        each<N, I + 1>(f);
+    }
+}
+
 template <int BM, int BN, int WM, int WN, int STAGES>
 struct Tile {
     static constexpr int kWavesM = BM / WM, kWavesN = BN / WN, kWaves = kWavesM * kWavesN, kThreads = 64 * kWaves;
@@ -181,6 +193,7 @@ struct TileParams {
     MatmulParams p;
     float* parts;            // [splits][M][N] partial sums, or NULL: the results themselves
     uint32_t tiles_m, splits, steps, steps_each;   // blocks of 128 in all, and of a split
+    bool quads;              // four scales of a row lie together, 16-byte aligned, in both matrices
     uint32_t band;           // tiles of A that neighbouring workgroups share out before they move along B
 };
 
@@ -207,7 +220,7 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
     const int64_t m0 = (int64_t)(band * t.band + in - along * high) * BM, n0 = (int64_t)along * BN;
     const uint32_t first = split * t.steps_each, last = min(first + t.steps_each, t.steps);
     const uint32_t whole = (uint32_t)(p.K / kGroup);                 // steps of 128 elements; at most one more is shorter
-    const uint32_t full = min(last, whole), n = full > first ? full - first : 0;
+    const uint32_t n = last > first ? last - first : 0;
 
     // rows past the end read the last one and are not stored
     const int64_t left_m = min(p.M - m0, (int64_t)BM) - 1, left_n = min(p.N - n0, (int64_t)BN) - 1;
@@ -217,14 +230,14 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
     const v4u rsa = uniform(resource(p.a.scale + m0 * p.a.scale_row_stride, 0xFFFFFFFFu));
     const v4u rsb = uniform(resource(p.b.scale + nb0 * p.b.scale_row_stride, 0xFFFFFFFFu));
     const uint32_t base = uniform((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds);
-    uint32_t off[T::kLoads];
-#pragma unroll
-    for (int i = 0; i < T::kLoads; ++i) {
-        const int row = (wave * T::kLoads + i) * 8 + (lane >> 3);
-        const uint32_t chunk = (lane & 7) ^ (row & 7);
-        off[i] = row < BM ? (uint32_t)(min((int64_t)row, left_m) * p.a.row_stride) + 16 * chunk
-                          : (uint32_t)(min((int64_t)(row - BM), left_n) * p.b.row_stride) + 16 * chunk;
-    }
+    // A wave's loads are of consecutive rows of one side, eight at a time: the first one's offset, and the last row's.
+    const bool codes_a = wave * T::kLoads * 8 < BM;
+    const int64_t code_stride = codes_a ? p.a.row_stride : p.b.row_stride;
+    const uint32_t row0 = wave * T::kLoads * 8 - (codes_a ? 0 : BM) + (lane >> 3), chunk = 16 * ((lane & 7) ^ (lane >> 3));
+    uint32_t off0 = row0 * (uint32_t)code_stride + chunk;
+    const uint32_t off_step = 8 * (uint32_t)code_stride;
+    const uint32_t off_last = (uint32_t)(codes_a ? left_m : left_n) * (uint32_t)code_stride + chunk;
+    const v4u rcodes = codes_a ? ra : rb;
     constexpr int kMine = (T::kSets + T::kWaves - 1) / T::kWaves;    // sets of scales of a wave
     uint32_t scale_off[kMine];
 #pragma unroll
@@ -234,12 +247,35 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
                                 : (uint32_t)(((n0 + min((int64_t)(row - BM), left_n)) / p.b.rows_per_scale - nb0) *
                                              p.b.scale_row_stride) * 4;
     }
-    auto fetch_step = [&](uint32_t s) {   // s: of this workgroup's steps
-        const uint32_t to = base + s % STAGES * T::kStage + wave * T::kLoads * 1024, at = (first + s) * kGroup;
+    // bytes from a row's scale to the next row's and the next block's, in LDS
+    const uint32_t by_row = t.quads ? 16 : 4, by_block = t.quads ? 4 : 4 * T::kRows;
+    // Loads FROM .. TO - 1 of a step (s: of this workgroup's steps).
+    auto fetch_codes = [&](uint32_t s, auto from, auto to) {
+        const uint32_t lds_to = base + s % STAGES * T::kStage + wave * T::kLoads * 1024, at = (first + s) * kGroup;
+        asm volatile("" : "+v"(off0));   // (the offsets are made anew each time, not held in registers)
 #pragma unroll
+        for (int i = from; i < to; ++i) fetch16(lds_to + i * 1024, rcodes, min(off0 + i * off_step, off_last), at);
+    };
+    // The last elements, less than 128, and zeros behind them.
+    auto copy_rest = [&](uint32_t s) {
+        const uint32_t lds_to = base + s % STAGES * T::kStage + wave * T::kLoads * 1024, at = (first + s) * kGroup;
+        const uint8_t* const codes = codes_a ? p.a.codes + m0 * p.a.row_stride : p.b.codes + n0 * p.b.row_stride;
+        const int64_t left = p.K - at - chunk;
+#pragma unroll 1
         for (int i = 0; i < T::kLoads; ++i) {
-            const bool of_a = (wave * T::kLoads + i) * 8 < BM;   // (uniform: a load's eight rows are of one side)
-            fetch16(to + i * 1024, of_a ? ra : rb, off[i], at);
+            const uint8_t* const from = codes + min(off0 + i * off_step, off_last) + at;
+            v4u v = {0, 0, 0, 0};
+            if (left >= 16) {
+                v = *reinterpret_cast<const v4u*>(from);
+            } else {
+#pragma unroll 1
+                for (int k = 0; k < left; ++k) {
+                    const uint32_t byte = (uint32_t)from[k] << (8 * (k & 3));
+                    v[0] |= k < 4 ? byte : 0, v[1] |= (k & 12) == 4 ? byte : 0;
+                    v[2] |= (k & 12) == 8 ? byte : 0, v[3] |= k >= 12 ? byte : 0;
+                }
+            }
+            *(__attribute__((address_space(3))) v4u*)(uintptr_t)(lds_to + i * 1024 + lane * 16) = v;
         }
     };
     auto fetch_scales = [&](uint32_t s) {   // of steps s .. s + 3, s a multiple of 4
@@ -248,11 +284,15 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
             const int set = wave + i * T::kWaves;
             if (set < T::kSets) {
                 const bool of_a = set * 64 < BM;
-                const uint32_t to = base + STAGES * T::kStage + ((s >> 2 & 1) * 4 * T::kRows + set * 64) * 4;
-                const uint32_t stride = (uint32_t)(of_a ? p.a.scale_block_stride : p.b.scale_block_stride) * 4;
+                const uint32_t to = base + STAGES * T::kStage + (s >> 2 & 1) * 16 * T::kRows + set * 64 * by_row;
+                if (t.quads) {
+                    fetch16(to, of_a ? rsa : rsb, scale_off[i], (first + s) * 4);
+                } else {
+                    const uint32_t stride = (uint32_t)(of_a ? p.a.scale_block_stride : p.b.scale_block_stride) * 4;
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (s + k < n) fetch4(to + k * T::kRows * 4, of_a ? rsa : rsb, scale_off[i], (first + s + k) * stride);
+                    for (int k = 0; k < 4; ++k)
+                        if (s + k < n) fetch4(to + k * by_block, of_a ? rsa : rsb, scale_off[i], (first + s + k) * stride);
+                }
             }
         }
     };
@@ -268,69 +308,104 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
             for (int r = 0; r < 4; ++r) acc[i][j][r] += d[r] * sa;   // (sa holds both)
         }
     };
-    if (n) {
-        fetch_scales(0);
-#pragma unroll
-        for (uint32_t s = 0; s < STAGES - 1; ++s)
-            if (s < n) fetch_step(s);
-    }
-    for (uint32_t s = 0; s < n; ++s) {
-        // step s is in LDS when the newest STAGES - 2 steps' loads may be left
-        if (s + STAGES - 1 <= n) drain<(STAGES - 2) * T::kLoads>();
-        else drain<0>();
+    // Addresses of this lane's codes in the first tile of its wave, of either side: chunk l / 16 of its row, and chunk l / 16 + 4
+    // 64 bytes before or behind. Tiles are 2048 bytes apart, steps kStage.
+    typedef const __attribute__((address_space(3))) v4u* Chunk;
+    typedef const __attribute__((address_space(3))) float* Number;
+    const uint32_t in_tile = col * kGroup + 16 * (quarter ^ (col & 7));
+    const uint32_t a_at = base + wm * kGroup + in_tile, b_at = base + (BM + wn) * kGroup + in_tile;
+    auto fragment = [&](uint32_t at, int tile) {
+        const v4u lo = *(Chunk)(uintptr_t)(at + tile * 2048), hi = *(Chunk)(uintptr_t)((at ^ 64) + tile * 2048);
+        return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    };
+    v8i b[NI], a[2];
+    v4f sb[NI] = {};
+    float sb1 = 1.f;
+    auto stage = [&](uint32_t s) { return s % STAGES * T::kStage; };
+    // A step's loads are spread over the tiles of A that follow the barrier which frees their buffer (the last two of a step and
+    // the first of the next), so that no wave is held up by a full queue of them: kIssued[x] of them after x of these tiles.
+    constexpr int kSlots = NJ >= 8 ? 6 : 4;
+    constexpr auto issued = [](int x) { return x >= kSlots ? T::kLoads : (x * T::kLoads + kSlots - 1) / kSlots; };
+    constexpr int kHead = issued(2);   // loads ahead of a step's end
+    const uint32_t loaded = min(last, whole) > first ? min(last, whole) - first : 0;   // steps that direct loads bring
+    // LEFT: the loads of step s - 1 + STAGES that the step before left; HEAD: the first of step s + STAGES.
+    auto step = [&](uint32_t s, auto LEFT, auto HEAD) {
         if ((s & 3) == 0 && s + 4 < n) fetch_scales(s + 4);
-        if (s + STAGES - 1 < n) fetch_step(s + STAGES - 1);
-        const uint8_t* const codes = lds + s % STAGES * T::kStage;
-        const float* const scales = reinterpret_cast<const float*>(lds + STAGES * T::kStage) + ((s >> 2 & 1) * 4 + (s & 3)) * T::kRows;
-        auto fragment = [&](int row) {
-            const uint8_t* const r = codes + row * kGroup;
-            const v4u lo = *reinterpret_cast<const v4u*>(r + 16 * (quarter ^ (row & 7)));
-            const v4u hi = *reinterpret_cast<const v4u*>(r + 16 * ((quarter + 4) ^ (row & 7)));
-            return v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-        };
-        v8i b[NI];
-        v4f sb[NI];
-        float sb1 = 1.f;
+        const uint32_t window = base + STAGES * T::kStage + (s >> 2 & 1) * 16 * T::kRows + (s & 3) * by_block;
+        uint32_t sa_at = window + (wm + col) * by_row;
+        if constexpr (BYROW) {
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            b[i] = fragment(BM + wn + 16 * i + col);
-            if constexpr (BYROW) sb[i] = *reinterpret_cast<const v4f*>(scales + BM + wn + 16 * i + 4 * quarter);
-            else sb[i] = v4f{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sb[i][r] = *(Number)(uintptr_t)(window + (BM + wn + 16 * i + 4 * quarter + r) * by_row);
+        } else {   // (WN rows of B from a multiple of WN share their scale)
+            sb1 = *(Number)(uintptr_t)(window + (BM + wn) * by_row);
         }
-        if constexpr (!BYROW) sb1 = scales[BM + wn];   // (WN rows of B from a multiple of WN share their scale)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const v8i a = fragment(wm + 16 * j + col);
-            const float sa = scales[wm + 16 * j + col] * sb1;
+        const uint32_t a_now = a_at + stage(s), a_then = a_at + stage(s + 1), b_then = b_at + stage(s + 1);
+        auto next_sa = [&] {
+            const float v = *(Number)(uintptr_t)sa_at;
+            sa_at += 16 * by_row;
+            asm volatile("" : "+v"(sa_at));   // (one running address)
+            return v;
+        };
+        float sa = next_sa(), sa_next = next_sa(), sa_last = 0.f;
+        auto tile = [&](auto J) {
+            constexpr int j = J;
+            if constexpr (j == NJ - 2) {
+                // The step's last two tiles are multiplied behind the barrier, from registers, while the next step's codes are
+                // read: step s + 1 is in LDS when the newest STAGES - 2 steps' loads may be left, and this step's buffer is free.
+                if constexpr (HEAD) drain<(STAGES - 2) * T::kLoads>();
+                else drain<0>();
+                if constexpr (LEFT && !HEAD)
+                    if (n > loaded) copy_rest(loaded);   // (s + STAGES)
+            }
+            if constexpr (HEAD && j >= NJ - 2)
+                fetch_codes(s + STAGES, Int<issued(j - NJ + 2)>(), Int<issued(j - NJ + 3)>());
+            if constexpr (LEFT && j + 2 < kSlots)
+                fetch_codes(s - 1 + STAGES, Int<issued(j + 2)>(), Int<issued(j + 3)>());
             v4f d[NI];
 #pragma unroll
-            for (int i = 0; i < NI; ++i) d[i] = dot128<WIDE>(b[i], a);
+            for (int i = 0; i < NI; ++i) {
+                d[i] = dot128<WIDE>(b[i], a[j & 1]);
+                if constexpr (j == NJ - 1) b[i] = fragment(b_then, i);   // (behind the last step: read and not used)
+            }
+            if constexpr (j + 2 < NJ) {
+                a[j & 1] = fragment(a_now, j + 2);
+                sa_last = next_sa();
+            } else {
+                a[j & 1] = fragment(a_then, j + 2 - NJ);
+            }
 #pragma unroll
-            for (int i = 0; i < NI; ++i) scaled(i, j, d[i], sa, sb[i]);
+            for (int i = 0; i < NI; ++i) {
+                scaled(i, j, d[i], sa * sb1, sb[i]);
+                asm volatile("" : "+v"(acc[i][j]));   // (added here: moved behind the branches, sums and products would not fit the registers)
+            }
+            sa = sa_next;
+            sa_next = sa_last;
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        each<NJ>(tile);
+    };
+    if (n) {
+        fetch_scales(0);
+        const bool ring = loaded >= STAGES;
+#pragma unroll
+        for (uint32_t s = 0; s < STAGES - 1; ++s)
+            if (s < loaded) fetch_codes(s, Int<0>(), Int<T::kLoads>());
+        if (ring) fetch_codes(STAGES - 1, Int<0>(), Int<kHead>());
+        else if (n > loaded) copy_rest(loaded);
+        if (ring) drain<(STAGES - 2) * T::kLoads + kHead>();
+        else drain<0>();
+#pragma unroll
+        for (int i = 0; i < NI; ++i) b[i] = fragment(b_at, i);
+        a[0] = fragment(a_at, 0);
+        a[1] = fragment(a_at, 1);
+        uint32_t s = 0;
+        if (ring) {
+            for (; s + STAGES < loaded; ++s) step(s, Int<1>(), Int<1>());
+            step(s++, Int<1>(), Int<0>());
         }
-    }
-    if (last > whole) {   // the last elements, less than 128
-        const int64_t k = (int64_t)whole * kGroup + 32 * quarter;
-        v8i b[NI];
-        v4f sb[NI];
-        const float* const scale = p.b.scale + whole * p.b.scale_block_stride;
-        float sb1 = 1.f;
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            b[i] = load32(p.b.codes + (n0 + min((int64_t)(wn + 16 * i + col), left_n)) * p.b.row_stride, k, p.K);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                sb[i][r] = BYROW ? scale[(n0 + min((int64_t)(wn + 16 * i + 4 * quarter + r), left_n)) * p.b.scale_row_stride] : 0.f;
-        }
-        if constexpr (!BYROW) sb1 = scale[(n0 + min((int64_t)wn, left_n)) / kGroup * p.b.scale_row_stride];
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int64_t m = m0 + min((int64_t)(wm + 16 * j + col), left_m);
-            const v8i a = load32(p.a.codes + m * p.a.row_stride, k, p.K);
-            const float sa = p.a.scale[m * p.a.scale_row_stride + whole * p.a.scale_block_stride] * sb1;
-#pragma unroll
-            for (int i = 0; i < NI; ++i) scaled(i, j, dot128<WIDE>(b[i], a), sa, sb[i]);
-        }
+        for (; s < n; ++s) step(s, Int<0>(), Int<0>());
     }
     // four consecutive results of a row each
     const bool quads = (p.out_stride & 3) == 0 && ((uintptr_t)p.out & (4 * sizeof(E) - 1)) == 0;
@@ -436,6 +511,7 @@ gvr_status gvr_fp8_matmul(const gvr_fp8_matrix* a, const gvr_fp8_matrix* b, int6
     t.steps = (uint32_t)gvr_fp8::groups_of(K);
     t.steps_each = (uint32_t)plan.steps_each;
     t.band = (uint32_t)plan.band;
+    t.quads = gvr_fp8::scale_quads(*a, K, plan.steps_each) && gvr_fp8::scale_quads(*b, K, plan.steps_each);
     return dtype == GVR_BF16 ? launch<__bf16>(t, plan, stream)
            : dtype == GVR_F16 ? launch<_Float16>(t, plan, stream) : launch<float>(t, plan, stream);
 }

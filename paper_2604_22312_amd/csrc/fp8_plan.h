@@ -110,6 +110,12 @@ inline bool tile_rows(const gvr_fp8_matrix& m, int rows, int64_t K) {
            (m.scale_row_stride * rows + m.scale_block_stride * groups_of(K)) * 4 < kMaxCount;
 }
 
+// Scales that 16-byte loads of four blocks can serve.
+inline bool scale_quads(const gvr_fp8_matrix& m, int64_t K, int64_t steps_each) {
+    return ((uintptr_t)m.scale & 15) == 0 && m.scale_block_stride == 1 && m.scale_row_stride % 4 == 0 &&
+           groups_of(K) % 4 == 0 && K % kGroup == 0 && steps_each % 4 == 0;
+}
+
 inline gvr_status plan_matmul(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, int64_t M, int64_t N, int64_t K, bool wide,
                               size_t ws_bytes, MatmulPlan* p) {
     const bool tiles = tile_rows(a, 256, K) && tile_rows(b, 256, K);
