@@ -143,6 +143,7 @@ __global__ __launch_bounds__(gvr_fp8::kThreads) void matmul_kernel(MatmulParams 
 // they write. drain<N>() waits until at most the newest N of them are under way,
 // and for every LDS read of the wave, ahead of the barrier after which buffers
 // change hands.
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
 DEV v4u resource(const void* base, uint32_t bytes) {
@@ -186,6 +187,7 @@ struct Tile {
     static constexpr int kSets = kRows / 64;                  // of 64 rows, whose scales a wave fetches at once
     static constexpr int kScales = 2 * 4 * kRows * 4;         // bytes: two windows of four blocks
     static constexpr int kLds = STAGES * kStage + kScales;
+    static_assert(WM % 32 == 0 && WN % 32 == 0, "tiles go in pairs");
     static_assert(kStage % (1024 * kWaves) == 0 && BM % 64 == 0 && BN % 64 == 0 && kSets <= 2 * kWaves, "");
 };
 
@@ -324,23 +326,25 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
     auto stage = [&](uint32_t s) { return s % STAGES * T::kStage; };
     // A step's loads are spread over the tiles of A that follow the barrier which frees their buffer (the last two of a step and
     // the first of the next), so that no wave is held up by a full queue of them: kIssued[x] of them after x of these tiles.
-    constexpr int kSlots = NJ >= 8 ? 6 : 4;
+    constexpr int kSlots = 4;
     constexpr auto issued = [](int x) { return x >= kSlots ? T::kLoads : (x * T::kLoads + kSlots - 1) / kSlots; };
     constexpr int kHead = issued(2);   // loads ahead of a step's end
     const uint32_t loaded = min(last, whole) > first ? min(last, whole) - first : 0;   // steps that direct loads bring
+    auto load_sb = [&](uint32_t window) {
+        if constexpr (BYROW)
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sb[i][r] = *(Number)(uintptr_t)(window + (BM + wn + 16 * i + 4 * quarter + r) * by_row);
+    };
+    v4f d[2][NI] = {};
+    float f_before = 0.f;
     // LEFT: the loads of step s - 1 + STAGES that the step before left; HEAD: the first of step s + STAGES.
     auto step = [&](uint32_t s, auto LEFT, auto HEAD) {
         if ((s & 3) == 0 && s + 4 < n) fetch_scales(s + 4);
         const uint32_t window = base + STAGES * T::kStage + (s >> 2 & 1) * 16 * T::kRows + (s & 3) * by_block;
         uint32_t sa_at = window + (wm + col) * by_row;
-        if constexpr (BYROW) {
-#pragma unroll
-            for (int i = 0; i < NI; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) sb[i][r] = *(Number)(uintptr_t)(window + (BM + wn + 16 * i + 4 * quarter + r) * by_row);
-        } else {   // (WN rows of B from a multiple of WN share their scale)
-            sb1 = *(Number)(uintptr_t)(window + (BM + wn) * by_row);
-        }
+        if constexpr (!BYROW) sb1 = *(Number)(uintptr_t)(window + (BM + wn) * by_row);   // (WN rows of B from a multiple of WN share it)
         const uint32_t a_now = a_at + stage(s), a_then = a_at + stage(s + 1), b_then = b_at + stage(s + 1);
         auto next_sa = [&] {
             const float v = *(Number)(uintptr_t)sa_at;
@@ -348,7 +352,7 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
             asm volatile("" : "+v"(sa_at));   // (one running address)
             return v;
         };
-        float sa = next_sa(), sa_next = next_sa(), sa_last = 0.f;
+        float sa = next_sa(), sa_next = next_sa();
         auto tile = [&](auto J) {
             constexpr int j = J;
             if constexpr (j == NJ - 2) {
@@ -363,26 +367,25 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
                 fetch_codes(s + STAGES, Int<issued(j - NJ + 2)>(), Int<issued(j - NJ + 3)>());
             if constexpr (LEFT && j + 2 < kSlots)
                 fetch_codes(s - 1 + STAGES, Int<issued(j + 2)>(), Int<issued(j + 3)>());
-            v4f d[NI];
+            // A tile's sums are scaled and added while the next one's are made, four additions to a matrix instruction: one wave's
+            // vector instructions run in the shadow of its own matrix instructions.
+            constexpr int before = (j + NJ - 1) % NJ;
+            const float f = sa * sb1;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
-                d[i] = dot128<WIDE>(b[i], a[j & 1]);
+                if (i == 0) __builtin_amdgcn_s_setprio(1);   // (the other wave of the unit is to read and add meanwhile)
+                d[j & 1][i] = dot128<WIDE>(b[i], a[j & 1]);
+                if (i == NI - 1) __builtin_amdgcn_s_setprio(0);
                 if constexpr (j == NJ - 1) b[i] = fragment(b_then, i);   // (behind the last step: read and not used)
+                if (i == NI - 1) a[j & 1] = j + 2 < NJ ? fragment(a_now, j + 2) : fragment(a_then, j + 2 - NJ);
+                scaled(i, before, d[(j + 1) & 1][i], f_before, sb[i]);
+                asm volatile("" : "+v"(acc[i][before]));   // (added here: moved behind the branches, sums and products would not fit the registers)
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if constexpr (j + 2 < NJ) {
-                a[j & 1] = fragment(a_now, j + 2);
-                sa_last = next_sa();
-            } else {
-                a[j & 1] = fragment(a_then, j + 2 - NJ);
-            }
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                scaled(i, j, d[i], sa * sb1, sb[i]);
-                asm volatile("" : "+v"(acc[i][j]));   // (added here: moved behind the branches, sums and products would not fit the registers)
-            }
+            f_before = f;
+            if constexpr (j == 0) load_sb(window);
             sa = sa_next;
-            sa_next = sa_last;
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (j + 2 < NJ) sa_next = next_sa();
         };
         each<NJ>(tile);
     };
@@ -406,31 +409,51 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
             step(s++, Int<1>(), Int<0>());
         }
         for (; s < n; ++s) step(s, Int<0>(), Int<0>());
+#pragma unroll
+        for (int i = 0; i < NI; ++i) scaled(i, NJ - 1, d[1][i], f_before, sb[i]);
     }
-    // four consecutive results of a row each
-    const bool quads = (p.out_stride & 3) == 0 && ((uintptr_t)p.out & (4 * sizeof(E) - 1)) == 0;
+    // A lane holds four consecutive results of a row in each tile; of 16-bit results two neighbouring tiles exchange lanes, so
+    // that it stores eight (8-byte stores cost the large product 18 us of 252).
+    typedef E e4 __attribute__((ext_vector_type(4)));
+    const bool rows16 = ((p.out_stride * (int)sizeof(E)) & 15) == 0 && ((uintptr_t)p.out & 15) == 0;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
         const int64_t m = m0 + wm + 16 * j + col;
+        if constexpr (sizeof(E) == 2) {
+            // (whole rows of lanes take part in the exchange, also those past the end)
+            if (!t.parts && rows16 && n0 + wn + WN <= p.N) {
+#pragma unroll
+                for (int i = 0; i < NI; i += 2) {
+                    const v2u x = __builtin_bit_cast(v2u, __builtin_convertvector(acc[i][j], e4));
+                    const v2u y = __builtin_bit_cast(v2u, __builtin_convertvector(acc[i + 1][j], e4));
+                    v4u r;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const auto s = __builtin_amdgcn_permlane32_swap(x[k], y[k], false, false);
+                        const auto q = __builtin_amdgcn_permlane16_swap(s[0], s[1], false, false);
+                        r[k] = q[0], r[2 + k] = q[1];
+                    }
+                    if (m < p.M)
+                        *reinterpret_cast<v4u*>(static_cast<E*>(p.out) + m * p.out_stride + n0 + wn + 16 * i + 8 * quarter) = r;
+                }
+                continue;
+            }
+        }
         if (m >= p.M) continue;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const int64_t c = n0 + wn + 16 * i + 4 * quarter;
-            if (t.parts) {
-                float* const to = t.parts + ((int64_t)split * p.M + m) * p.N + c;
+            float* const part = t.parts ? t.parts + ((int64_t)split * p.M + m) * p.N + c : nullptr;
+            E* const to = static_cast<E*>(p.out) + m * p.out_stride + c;
+            if (!part && sizeof(E) == 4 && rows16 && c + 3 < p.N) {
+                *reinterpret_cast<e4*>(to) = __builtin_convertvector(acc[i][j], e4);
+            } else {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (c + r < p.N) to[r] = acc[i][j][r];
-            } else {
-                E* const to = static_cast<E*>(p.out) + m * p.out_stride + c;
-                typedef E e4 __attribute__((ext_vector_type(4)));
-                if (quads && c + 3 < p.N) {
-                    *reinterpret_cast<e4*>(to) = __builtin_convertvector(acc[i][j], e4);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (c + r < p.N) to[r] = (E)acc[i][j][r];
-                }
+                    if (c + r < p.N) {
+                        if (part) part[r] = acc[i][j][r];
+                        else to[r] = (E)acc[i][j][r];
+                    }
             }
         }
     }
