@@ -187,6 +187,7 @@ struct Tile {
     static constexpr int kSets = kRows / 64;                  // of 64 rows, whose scales a wave fetches at once
     static constexpr int kScales = 2 * 4 * kRows * 4;         // bytes: two windows of four blocks
     static constexpr int kLds = STAGES * kStage + kScales;
+    static_assert(STAGES <= 5, "scales come four steps ahead");
     static_assert(WM % 32 == 0 && WN % 32 == 0, "tiles go in pairs");
     static_assert(kStage % (1024 * kWaves) == 0 && BM % 64 == 0 && BN % 64 == 0 && kSets <= 2 * kWaves, "");
 };
@@ -195,6 +196,7 @@ struct TileParams {
     MatmulParams p;
     float* parts;            // [splits][M][N] partial sums, or NULL: the results themselves
     uint32_t tiles_m, splits, steps, steps_each;   // blocks of 128 in all, and of a split
+    uint32_t join_cols;      // workgroups of a row of results in the kernel that adds the parts
     bool quads;              // four scales of a row lie together, 16-byte aligned, in both matrices
     uint32_t band;           // tiles of A that neighbouring workgroups share out before they move along B
 };
@@ -258,26 +260,27 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
 #pragma unroll
         for (int i = from; i < to; ++i) fetch16(lds_to + i * 1024, rcodes, min(off0 + i * off_step, off_last), at);
     };
-    // The last elements, less than 128, and zeros behind them.
+    // The last elements, less than 128, and zeros behind them: whole chunks first, then the one that ends inside (a lane a row).
     auto copy_rest = [&](uint32_t s) {
         const uint32_t lds_to = base + s % STAGES * T::kStage + wave * T::kLoads * 1024, at = (first + s) * kGroup;
-        const uint8_t* const codes = codes_a ? p.a.codes + m0 * p.a.row_stride : p.b.codes + n0 * p.b.row_stride;
-        const int64_t left = p.K - at - chunk;
-#pragma unroll 1
+        const uint8_t* const codes = (codes_a ? p.a.codes + m0 * p.a.row_stride : p.b.codes + n0 * p.b.row_stride) + at;
+        const int left = (int)(p.K - at), mine = left - (int)chunk;
+        v4u v[T::kLoads];
+#pragma unroll
         for (int i = 0; i < T::kLoads; ++i) {
-            const uint8_t* const from = codes + min(off0 + i * off_step, off_last) + at;
-            v4u v = {0, 0, 0, 0};
-            if (left >= 16) {
-                v = *reinterpret_cast<const v4u*>(from);
-            } else {
-#pragma unroll 1
-                for (int k = 0; k < left; ++k) {
-                    const uint32_t byte = (uint32_t)from[k] << (8 * (k & 3));
-                    v[0] |= k < 4 ? byte : 0, v[1] |= (k & 12) == 4 ? byte : 0;
-                    v[2] |= (k & 12) == 8 ? byte : 0, v[3] |= k >= 12 ? byte : 0;
-                }
-            }
-            *(__attribute__((address_space(3))) v4u*)(uintptr_t)(lds_to + i * 1024 + lane * 16) = v;
+            v[i] = v4u{0, 0, 0, 0};
+            if (mine >= 16) v[i] = *reinterpret_cast<const v4u*>(codes + min(off0 + i * off_step, off_last));
+        }
+#pragma unroll
+        for (int i = 0; i < T::kLoads; ++i) *(__attribute__((address_space(3))) v4u*)(uintptr_t)(lds_to + i * 1024 + lane * 16) = v[i];
+        if ((left & 15) && lane < 8 * T::kLoads) {
+            const int64_t row = wave * T::kLoads * 8 - (codes_a ? 0 : BM) + lane;
+            const uint8_t* const from = codes + min(row, codes_a ? left_m : left_n) * code_stride + (left & ~15);
+            v4u w = {0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < 15; ++k)
+                if (k < (left & 15)) w[k / 4] |= (uint32_t)from[k] << (8 * (k & 3));
+            *(__attribute__((address_space(3))) v4u*)(uintptr_t)(lds_to + lane * 128 + 16 * ((left >> 4) ^ (lane & 7))) = w;
         }
     };
     auto fetch_scales = [&](uint32_t s) {   // of steps s .. s + 3, s a multiple of 4
@@ -445,7 +448,9 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
             const int64_t c = n0 + wn + 16 * i + 4 * quarter;
             float* const part = t.parts ? t.parts + ((int64_t)split * p.M + m) * p.N + c : nullptr;
             E* const to = static_cast<E*>(p.out) + m * p.out_stride + c;
-            if (!part && sizeof(E) == 4 && rows16 && c + 3 < p.N) {
+            if (part && (p.N & 3) == 0) {
+                if (c < p.N) *reinterpret_cast<v4f*>(part) = acc[i][j];
+            } else if (!part && sizeof(E) == 4 && rows16 && c + 3 < p.N) {
                 *reinterpret_cast<e4*>(to) = __builtin_convertvector(acc[i][j], e4);
             } else {
 #pragma unroll
@@ -459,40 +464,170 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
     }
 }
 
-// Sums of the splits' parts, in their order.
+// --- few rows of A
+//
+// A workgroup multiplies 16 NT rows of B with 16 MT rows of A; its waves share out
+// the blocks of 128 and their sums are added at the end, in the order of the waves.
+// Codes go from memory to registers (B's once, A's from L2 for every workgroup),
+// AHEAD blocks of a wave at a time, with no barrier on the way. Lane l holds chunks
+// l / 16 and l / 16 + 4 of its rows.
+
+// Chunks `quarter` and `quarter` + 4 of a row's 128 bytes from k on, zeros past K.
+DEV v8i load_chunks(const uint8_t* row, int64_t k, int64_t K, int quarter, bool whole) {
+    v4u v[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t at = k + 64 * h + 16 * quarter, left = K - at;
+        if (whole || left >= 16) {
+            v[h] = *reinterpret_cast<const v4u*>(row + at);
+        } else {
+            v[h] = v4u{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (i < left) v[h][i / 4] |= (uint32_t)row[at + i] << (8 * (i & 3));
+        }
+    }
+    return v8i{(int)v[0][0], (int)v[0][1], (int)v[0][2], (int)v[0][3], (int)v[1][0], (int)v[1][1], (int)v[1][2], (int)v[1][3]};
+}
+
+template <class E, bool BYROW, int MT, int NT, int AHEAD, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void rows_kernel(MatmulParams p) {
+    constexpr bool WIDE = sizeof(E) == 4;
+    __shared__ v4f sums[WAVES][MT][64];
+    const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
+    const int64_t n0 = (int64_t)(blockIdx.x % p.tiles_n) * (16 * NT), m0 = (int64_t)(blockIdx.x / p.tiles_n) * (16 * MT);
+    // rows past the end read the last one and are not stored
+    const uint8_t* const a = p.a.codes + m0 * p.a.row_stride;
+    const uint8_t* const b = p.b.codes + n0 * p.b.row_stride;
+    const int64_t nb0 = n0 / p.b.rows_per_scale;
+    const float* const sa = p.a.scale + m0 * p.a.scale_row_stride;
+    const float* const sb = p.b.scale + nb0 * p.b.scale_row_stride;
+    uint32_t a_row[MT], b_row[NT], sa_row[MT], sb_row[BYROW ? 4 * NT : 1];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+        const uint32_t m = (uint32_t)min((int64_t)(16 * j + col), p.M - m0 - 1);
+        a_row[j] = m * (uint32_t)p.a.row_stride;
+        sa_row[j] = m * (uint32_t)p.a.scale_row_stride;
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        b_row[i] = (uint32_t)min((int64_t)(16 * i + col), p.N - n0 - 1) * (uint32_t)p.b.row_stride;
+        if constexpr (BYROW)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                sb_row[4 * i + r] = (uint32_t)min((int64_t)(16 * i + 4 * quarter + r), p.N - n0 - 1) * (uint32_t)p.b.scale_row_stride;
+    }
+    if constexpr (!BYROW) sb_row[0] = 0;   // (16 NT rows from a multiple of 16 NT share their scale)
+    v4f acc[NT][MT] = {};
+    const int64_t steps = (p.K + kGroup - 1) / kGroup;
+    for (int64_t s0 = wave; s0 < steps; s0 += WAVES * AHEAD) {
+        v8i bv[AHEAD][NT], av[AHEAD][MT];
+        float fa[AHEAD][MT], fb[AHEAD][BYROW ? 4 * NT : 1];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int64_t s = s0 + u * WAVES;
+            if (s < steps) {
+                const bool whole = (s + 1) * kGroup <= p.K;
+#pragma unroll
+                for (int i = 0; i < NT; ++i) bv[u][i] = load_chunks(b + b_row[i], s * kGroup, p.K, quarter, whole);
+#pragma unroll
+                for (int i = 0; i < (BYROW ? 4 * NT : 1); ++i) fb[u][i] = sb[sb_row[i] + s * p.b.scale_block_stride];
+#pragma unroll
+                for (int j = 0; j < MT; ++j) {
+                    av[u][j] = load_chunks(a + a_row[j], s * kGroup, p.K, quarter, whole);
+                    fa[u][j] = sa[sa_row[j] + s * p.a.scale_block_stride];
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (s0 + u * WAVES < steps) {
+#pragma unroll
+                for (int j = 0; j < MT; ++j)
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        const v4f d = dot128<WIDE>(bv[u][i], av[u][j]);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[i][j][r] += d[r] * (fa[u][j] * fb[u][BYROW ? 4 * i + r : 0]);
+                    }
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        if (i) __syncthreads();
+#pragma unroll
+        for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[i][j];
+        __syncthreads();
+        for (int at = threadIdx.x; at < MT * 64; at += 64 * WAVES) {
+            const int j = at >> 6, l = at & 63;
+            v4f sum = sums[0][j][l];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) {
+                const v4f v = sums[w][j][l];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[r] += v[r];
+            }
+            const int64_t m = m0 + 16 * j + (l & 15), n = n0 + 16 * i + 4 * (l >> 4);
+            if (m < p.M) {
+                E* const to = static_cast<E*>(p.out) + m * p.out_stride + n;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (n + r < p.N) to[r] = (E)sum[r];
+            }
+        }
+    }
+}
+
+// Sums of the splits' parts, in their order; a thread takes four results of a row, a workgroup 1024.
 template <class E>
 __global__ __launch_bounds__(gvr_fp8::kThreads) void join_kernel(TileParams t) {
     const MatmulParams& p = t.p;
-    const int64_t at = (int64_t)blockIdx.x * gvr_fp8::kThreads + threadIdx.x, total = p.M * p.N;
-    if (at >= total) return;
-    float sum = 0.f;
-    for (uint32_t s = 0; s < t.splits; ++s) sum += t.parts[s * total + at];
-    const int64_t m = at / p.N, n = at - m * p.N;
-    static_cast<E*>(p.out)[m * p.out_stride + n] = (E)sum;
+    const int64_t m = blockIdx.x / t.join_cols, n = ((int64_t)(blockIdx.x % t.join_cols) * gvr_fp8::kThreads + threadIdx.x) * 4;
+    if (n >= p.N) return;
+    const int64_t total = p.M * p.N;
+    const float* from = t.parts + m * p.N + n;
+    E* const to = static_cast<E*>(p.out) + m * p.out_stride + n;
+    v4f sum = {0.f, 0.f, 0.f, 0.f};
+    if ((p.N & 3) == 0) {
+        for (uint32_t s = 0; s < t.splits; ++s, from += total) sum += *reinterpret_cast<const v4f*>(from);
+    } else {
+        for (uint32_t s = 0; s < t.splits; ++s, from += total)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (n + r < p.N) sum[r] += from[r];
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (n + r < p.N) to[r] = (E)sum[r];
+}
+
+template <class E, bool BYROW>
+void launch_shape(const TileParams& t, const gvr_fp8::MatmulPlan& plan, hipStream_t s) {
+    const dim3 grid((unsigned)plan.workgroups), block(plan.threads);
+    auto go = [&](auto kernel, auto params) { hipLaunchKernelGGL(kernel, grid, block, 0, s, params); };
+    switch (plan.shape) {
+        case gvr_fp8::kAnyShape: go(matmul_kernel<E>, t.p); break;
+        case gvr_fp8::kRows16: plan.threads == 512 ? go(rows_kernel<E, BYROW, 1, 1, 4, 8>, t.p) : go(rows_kernel<E, BYROW, 1, 1, 4, 16>, t.p); break;
+        case gvr_fp8::kRows32: go(rows_kernel<E, BYROW, 2, 1, 4, 8>, t.p); break;
+        case gvr_fp8::kRows64: go(rows_kernel<E, BYROW, 4, 1, 2, 8>, t.p); break;
+        case gvr_fp8::kRows64x2: go(rows_kernel<E, BYROW, 4, 2, 2, 8>, t.p); break;
+        case gvr_fp8::kRows128: go(rows_kernel<E, BYROW, 8, 1, 2, 8>, t.p); break;
+        case gvr_fp8::kRows128x2: go(rows_kernel<E, BYROW, 8, 2, 1, 8>, t.p); break;
+        case gvr_fp8::kLow: go(tile_kernel<E, BYROW, 64, 128, 64, 32, 5>, t); break;
+        case gvr_fp8::kNarrow: go(tile_kernel<E, BYROW, 128, 64, 64, 32, 5>, t); break;
+        case gvr_fp8::kSquare: go(tile_kernel<E, BYROW, 128, 128, 64, 64, 2>, t); break;
+        case gvr_fp8::kLarge:
+            if constexpr (sizeof(E) == 2) go(tile_kernel<E, BYROW, 256, 256, 128, 64, 2>, t);
+            break;
+    }
 }
 
 template <class E>
 gvr_status launch(const TileParams& t, const gvr_fp8::MatmulPlan& plan, void* stream) {
-    const dim3 grid((unsigned)plan.workgroups);
     const hipStream_t s = (hipStream_t)stream;
-    const bool by_row = t.p.b.rows_per_scale == 1;
-    switch (plan.shape) {
-        case gvr_fp8::kAnyShape:
-            hipLaunchKernelGGL(matmul_kernel<E>, grid, dim3(gvr_fp8::kThreads), 0, s, t.p);
-            break;
-        case gvr_fp8::kLarge:
-            if constexpr (sizeof(E) == 2) {
-                if (by_row) hipLaunchKernelGGL((tile_kernel<E, true, 256, 256, 128, 64, 2>), grid, dim3(512), 0, s, t);
-                else hipLaunchKernelGGL((tile_kernel<E, false, 256, 256, 128, 64, 2>), grid, dim3(512), 0, s, t);
-            }
-            break;
-        default:
-            if (by_row) hipLaunchKernelGGL((tile_kernel<E, true, 128, 128, 64, 64, 2>), grid, dim3(256), 0, s, t);
-            else hipLaunchKernelGGL((tile_kernel<E, false, 128, 128, 64, 64, 2>), grid, dim3(256), 0, s, t);
-    }
+    t.p.b.rows_per_scale == 1 ? launch_shape<E, true>(t, plan, s) : launch_shape<E, false>(t, plan, s);
     if (t.parts)
-        hipLaunchKernelGGL(join_kernel<E>, dim3((unsigned)((t.p.M * t.p.N + gvr_fp8::kThreads - 1) / gvr_fp8::kThreads)),
-                           dim3(gvr_fp8::kThreads), 0, s, t);
+        hipLaunchKernelGGL(join_kernel<E>, dim3((unsigned)(t.p.M * t.join_cols)), dim3(gvr_fp8::kThreads), 0, s, t);
     return hipGetLastError() == hipSuccess ? GVR_OK : GVR_ERR_HIP;
 }
 
@@ -532,6 +667,7 @@ gvr_status gvr_fp8_matmul(const gvr_fp8_matrix* a, const gvr_fp8_matrix* b, int6
     t.tiles_m = (uint32_t)plan.tiles_m;
     t.splits = (uint32_t)plan.splits;
     t.steps = (uint32_t)gvr_fp8::groups_of(K);
+    t.join_cols = (uint32_t)((N + 4 * gvr_fp8::kThreads - 1) / (4 * gvr_fp8::kThreads));
     t.steps_each = (uint32_t)plan.steps_each;
     t.band = (uint32_t)plan.band;
     t.quads = gvr_fp8::scale_quads(*a, K, plan.steps_each) && gvr_fp8::scale_quads(*b, K, plan.steps_each);

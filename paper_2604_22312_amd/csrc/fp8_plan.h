@@ -91,12 +91,30 @@ inline gvr_status check_matmul(const gvr_fp8_matrix* a, const gvr_fp8_matrix* b,
     return GVR_OK;
 }
 
-constexpr int kTileM = 64, kTileN = 64, kThreads = 256;
-enum Shape { kAnyShape, kLarge, kSquare };
+constexpr int kTileM = 64, kTileN = 64, kThreads = 256;   // of the kernel that takes any alignment
+enum Shape { kAnyShape, kRows16, kRows32, kRows64, kRows64x2, kRows128, kRows128x2, kLow, kNarrow, kSquare, kLarge };
+struct Tiles {
+    int m, n, threads;   // rows of A and of B of a workgroup
+};
+inline Tiles tiles_of(Shape s) {
+    switch (s) {
+        case kRows16: return {16, 16, 512};
+        case kRows32: return {32, 16, 512};
+        case kRows64: return {64, 16, 512};
+        case kRows64x2: return {64, 32, 512};
+        case kRows128: return {128, 16, 512};
+        case kRows128x2: return {128, 32, 512};
+        case kLow: return {64, 128, 256};
+        case kNarrow: return {128, 64, 256};
+        case kSquare: return {128, 128, 256};
+        case kLarge: return {256, 256, 512};
+        default: return {kTileM, kTileN, kThreads};
+    }
+}
 
 struct MatmulPlan {
     Shape shape;
-    int tile_m, tile_n, threads;
+    int threads;
     int64_t tiles_m, tiles_n, splits, steps_each, band, workgroups;
     size_t workspace;   // bytes of the splits' parts
 };
@@ -119,15 +137,21 @@ inline bool scale_quads(const gvr_fp8_matrix& m, int64_t K, int64_t steps_each) 
 inline gvr_status plan_matmul(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, int64_t M, int64_t N, int64_t K, bool wide,
                               size_t ws_bytes, MatmulPlan* p) {
     const bool tiles = tile_rows(a, 256, K) && tile_rows(b, 256, K);
-    p->shape = !tiles ? kAnyShape : !wide && M * N >= (int64_t)256 * 256 * 128 ? kLarge : kSquare;
-    p->tile_m = p->tile_n = p->shape == kLarge ? 256 : p->shape == kSquare ? 128 : 64;
-    p->threads = p->shape == kLarge ? 512 : 256;
-    p->tiles_m = (M + p->tile_m - 1) / p->tile_m;
-    p->tiles_n = (N + p->tile_n - 1) / p->tile_n;   // (each at most 2^25)
-    p->splits = 1;
-    p->steps_each = groups_of(K);
+    p->shape = !tiles ? kAnyShape : M <= 16 ? kRows16 : M <= 32 ? kRows32 : !wide && M * N >= (int64_t)256 * 256 * 128 ? kLarge : kSquare;
+    const Tiles t = tiles_of(p->shape);
+    p->threads = t.threads;
+    p->tiles_m = (M + t.m - 1) / t.m;
+    p->tiles_n = (N + t.n - 1) / t.n;   // (each at most 2^27)
+    if (p->shape == kRows16 && p->tiles_n < 256) p->threads = 1024;
+    int64_t steps = groups_of(K), splits = 1;
+    // SWEEP
+    p->steps_each = (steps + splits - 1) / splits;
+    if (splits > 1) p->steps_each = (p->steps_each + 3) / 4 * 4;
+    p->splits = p->steps_each ? (steps + p->steps_each - 1) / p->steps_each : 1;
+    if (p->splits < 1) p->splits = 1;
     p->band = 8;
-    p->workspace = 0;
+    p->workspace = p->splits > 1 ? (size_t)p->splits * M * N * 4 : 0;
+    if (p->workspace > ws_bytes) p->splits = 1, p->steps_each = steps, p->workspace = 0;
     p->workgroups = p->tiles_m * p->tiles_n * p->splits;
     return p->workgroups * p->threads > 0xFFFFFFFFll ? GVR_ERR_TOO_LONG : GVR_OK;
 }
