@@ -183,13 +183,13 @@ struct Tile {
     static constexpr int kWavesM = BM / WM, kWavesN = BN / WN, kWaves = kWavesM * kWavesN, kThreads = 64 * kWaves;
     static constexpr int kRows = BM + BN;
     static constexpr int kStage = kRows * kGroup;             // bytes of a step's codes
-    static constexpr int kLoads = kStage / 1024 / kWaves;     // of a wave and step
+    static constexpr int kLoadsA = BM / 8 / kWaves, kLoadsB = BN / 8 / kWaves, kLoads = kLoadsA + kLoadsB;   // of a wave and step
     static constexpr int kSets = kRows / 64;                  // of 64 rows, whose scales a wave fetches at once
     static constexpr int kScales = 2 * 4 * kRows * 4;         // bytes: two windows of four blocks
     static constexpr int kLds = STAGES * kStage + kScales;
     static_assert(STAGES <= 5, "scales come four steps ahead");
     static_assert(WM % 32 == 0 && WN % 32 == 0, "tiles go in pairs");
-    static_assert(kStage % (1024 * kWaves) == 0 && BM % 64 == 0 && BN % 64 == 0 && kSets <= 2 * kWaves, "");
+    static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && BM % 64 == 0 && BN % 64 == 0 && kLoads <= 8, "");
 };
 
 struct TileParams {
@@ -234,14 +234,16 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
     const v4u rsa = uniform(resource(p.a.scale + m0 * p.a.scale_row_stride, 0xFFFFFFFFu));
     const v4u rsb = uniform(resource(p.b.scale + nb0 * p.b.scale_row_stride, 0xFFFFFFFFu));
     const uint32_t base = uniform((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds);
-    // A wave's loads are of consecutive rows of one side, eight at a time: the first one's offset, and the last row's.
-    const bool codes_a = wave * T::kLoads * 8 < BM;
-    const int64_t code_stride = codes_a ? p.a.row_stride : p.b.row_stride;
-    const uint32_t row0 = wave * T::kLoads * 8 - (codes_a ? 0 : BM) + (lane >> 3), chunk = 16 * ((lane & 7) ^ (lane >> 3));
-    uint32_t off0 = row0 * (uint32_t)code_stride + chunk;
-    const uint32_t off_step = 8 * (uint32_t)code_stride;
-    const uint32_t off_last = (uint32_t)(codes_a ? left_m : left_n) * (uint32_t)code_stride + chunk;
-    const v4u rcodes = codes_a ? ra : rb;
+    // A wave's loads are of eight consecutive rows each, first kLoadsA of A's, then of B's: the first ones' offsets, and the last rows'.
+    const uint32_t chunk = 16 * ((lane & 7) ^ (lane >> 3)), a_stride = (uint32_t)p.a.row_stride, b_stride = (uint32_t)p.b.row_stride;
+    uint32_t off_a = (wave * T::kLoadsA * 8 + (lane >> 3)) * a_stride + chunk, off_b = (wave * T::kLoadsB * 8 + (lane >> 3)) * b_stride + chunk;
+    const uint32_t last_a = (uint32_t)left_m * a_stride + chunk, last_b = (uint32_t)left_n * b_stride + chunk;
+    auto load_offset = [&](int i) {
+        return i < T::kLoadsA ? min(off_a + i * 8 * a_stride, last_a) : min(off_b + (i - T::kLoadsA) * 8 * b_stride, last_b);
+    };
+    auto load_place = [&](int i) {   // in a buffer
+        return (uint32_t)(i < T::kLoadsA ? wave * T::kLoadsA + i : BM / 8 + wave * T::kLoadsB + i - T::kLoadsA) * 1024;
+    };
     constexpr int kMine = (T::kSets + T::kWaves - 1) / T::kWaves;    // sets of scales of a wave
     uint32_t scale_off[kMine];
 #pragma unroll
@@ -254,33 +256,35 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
     // bytes from a row's scale to the next row's and the next block's, in LDS
     const uint32_t by_row = t.quads ? 16 : 4, by_block = t.quads ? 4 : 4 * T::kRows;
     // Loads FROM .. TO - 1 of a step (s: of this workgroup's steps).
-    auto fetch_codes = [&](uint32_t s, auto from, auto to) {
-        const uint32_t lds_to = base + s % STAGES * T::kStage + wave * T::kLoads * 1024, at = (first + s) * kGroup;
-        asm volatile("" : "+v"(off0));   // (the offsets are made anew each time, not held in registers)
+    auto fetch_codes = [&](uint32_t s, auto FROM, auto TO) {
+        const uint32_t lds_to = base + s % STAGES * T::kStage, at = (first + s) * kGroup;
+        asm volatile("" : "+v"(off_a), "+v"(off_b));   // (the offsets are made anew each time, not held in registers)
 #pragma unroll
-        for (int i = from; i < to; ++i) fetch16(lds_to + i * 1024, rcodes, min(off0 + i * off_step, off_last), at);
+        for (int i = FROM; i < TO; ++i) fetch16(lds_to + load_place(i), i < T::kLoadsA ? ra : rb, load_offset(i), at);
     };
     // The last elements, less than 128, and zeros behind them: whole chunks first, then the one that ends inside (a lane a row).
     auto copy_rest = [&](uint32_t s) {
-        const uint32_t lds_to = base + s % STAGES * T::kStage + wave * T::kLoads * 1024, at = (first + s) * kGroup;
-        const uint8_t* const codes = (codes_a ? p.a.codes + m0 * p.a.row_stride : p.b.codes + n0 * p.b.row_stride) + at;
+        const uint32_t lds_to = base + s % STAGES * T::kStage, at = (first + s) * kGroup;
+        const uint8_t *const codes_a = p.a.codes + m0 * p.a.row_stride + at, *const codes_b = p.b.codes + n0 * p.b.row_stride + at;
         const int left = (int)(p.K - at), mine = left - (int)chunk;
         v4u v[T::kLoads];
 #pragma unroll
         for (int i = 0; i < T::kLoads; ++i) {
             v[i] = v4u{0, 0, 0, 0};
-            if (mine >= 16) v[i] = *reinterpret_cast<const v4u*>(codes + min(off0 + i * off_step, off_last));
+            if (mine >= 16) v[i] = *reinterpret_cast<const v4u*>((i < T::kLoadsA ? codes_a : codes_b) + load_offset(i));
         }
 #pragma unroll
-        for (int i = 0; i < T::kLoads; ++i) *(__attribute__((address_space(3))) v4u*)(uintptr_t)(lds_to + i * 1024 + lane * 16) = v[i];
+        for (int i = 0; i < T::kLoads; ++i) *(__attribute__((address_space(3))) v4u*)(uintptr_t)(lds_to + load_place(i) + lane * 16) = v[i];
         if ((left & 15) && lane < 8 * T::kLoads) {
-            const int64_t row = wave * T::kLoads * 8 - (codes_a ? 0 : BM) + lane;
-            const uint8_t* const from = codes + min(row, codes_a ? left_m : left_n) * code_stride + (left & ~15);
+            const bool of_a = lane < 8 * T::kLoadsA;
+            const int row = of_a ? wave * T::kLoadsA * 8 + lane : wave * T::kLoadsB * 8 + lane - 8 * T::kLoadsA;
+            const uint8_t* const from = (of_a ? codes_a + min((int64_t)row, left_m) * a_stride
+                                              : codes_b + min((int64_t)row, left_n) * b_stride) + (left & ~15);
             v4u w = {0, 0, 0, 0};
 #pragma unroll
             for (int k = 0; k < 15; ++k)
                 if (k < (left & 15)) w[k / 4] |= (uint32_t)from[k] << (8 * (k & 3));
-            *(__attribute__((address_space(3))) v4u*)(uintptr_t)(lds_to + lane * 128 + 16 * ((left >> 4) ^ (lane & 7))) = w;
+            *(__attribute__((address_space(3))) v4u*)(uintptr_t)(lds_to + (of_a ? row : BM + row) * 128 + 16 * ((left >> 4) ^ (row & 7))) = w;
         }
     };
     auto fetch_scales = [&](uint32_t s) {   // of steps s .. s + 3, s a multiple of 4
@@ -464,116 +468,103 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
     }
 }
 
-// --- few rows of A
+// --- up to 16 rows of A
 //
-// A workgroup multiplies 16 NT rows of B with 16 MT rows of A; its waves share out
-// the blocks of 128 and their sums are added at the end, in the order of the waves.
-// Codes go from memory to registers (B's once, A's from L2 for every workgroup),
-// AHEAD blocks of a wave at a time, with no barrier on the way. Lane l holds chunks
-// l / 16 and l / 16 + 4 of its rows.
+// A workgroup multiplies 16 NT rows of B with all rows of A; its waves share out the
+// blocks of 128 and their sums are added at the end, in the order of the waves. Codes
+// go from memory to registers, kAhead blocks of a wave at a time, with no barrier on
+// the way. Lane l holds chunks l / 16 and l / 16 + 4 of its rows.
+constexpr int kAhead = 4;
 
-// Chunks `quarter` and `quarter` + 4 of a row's 128 bytes from k on, zeros past K.
-DEV v8i load_chunks(const uint8_t* row, int64_t k, int64_t K, int quarter, bool whole) {
+// Chunks `quarter` and `quarter` + 4 of a row's 128 bytes; REST: of the last ones, zeros past `left`.
+template <bool REST>
+DEV v8i load_chunks(const uint8_t* row, int quarter, int left) {
     v4u v[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int64_t at = k + 64 * h + 16 * quarter, left = K - at;
-        if (whole || left >= 16) {
+        const int at = 64 * h + 16 * quarter;
+        if (!REST || left >= at + 16) {
             v[h] = *reinterpret_cast<const v4u*>(row + at);
         } else {
             v[h] = v4u{0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (i < left) v[h][i / 4] |= (uint32_t)row[at + i] << (8 * (i & 3));
+            for (int i = 0; i < 15; ++i)
+                if (at + i < left) v[h][i / 4] |= (uint32_t)row[at + i] << (8 * (i & 3));
         }
     }
     return v8i{(int)v[0][0], (int)v[0][1], (int)v[0][2], (int)v[0][3], (int)v[1][0], (int)v[1][1], (int)v[1][2], (int)v[1][3]};
 }
 
-template <class E, bool BYROW, int MT, int NT, int AHEAD, int WAVES>
+template <class E, bool BYROW, int NT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void rows_kernel(MatmulParams p) {
     constexpr bool WIDE = sizeof(E) == 4;
-    __shared__ v4f sums[WAVES][MT][64];
+    __shared__ v4f sums[WAVES][NT][64];
     const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
-    const int64_t n0 = (int64_t)(blockIdx.x % p.tiles_n) * (16 * NT), m0 = (int64_t)(blockIdx.x / p.tiles_n) * (16 * MT);
-    // rows past the end read the last one and are not stored
-    const uint8_t* const a = p.a.codes + m0 * p.a.row_stride;
-    const uint8_t* const b = p.b.codes + n0 * p.b.row_stride;
-    const int64_t nb0 = n0 / p.b.rows_per_scale;
-    const float* const sa = p.a.scale + m0 * p.a.scale_row_stride;
-    const float* const sb = p.b.scale + nb0 * p.b.scale_row_stride;
-    uint32_t a_row[MT], b_row[NT], sa_row[MT], sb_row[BYROW ? 4 * NT : 1];
-#pragma unroll
-    for (int j = 0; j < MT; ++j) {
-        const uint32_t m = (uint32_t)min((int64_t)(16 * j + col), p.M - m0 - 1);
-        a_row[j] = m * (uint32_t)p.a.row_stride;
-        sa_row[j] = m * (uint32_t)p.a.scale_row_stride;
-    }
+    const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
+    // rows of B past the end read the last one and are not stored, those of A are zeros
+    const bool of_a = col < p.M;
+    const uint8_t* const a = p.a.codes + (of_a ? col : 0) * p.a.row_stride;
+    const float* const sa = p.a.scale + (of_a ? col : 0) * p.a.scale_row_stride;
+    const uint8_t* b[NT];
+    const float* sb[BYROW ? 4 * NT : 1];
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        b_row[i] = (uint32_t)min((int64_t)(16 * i + col), p.N - n0 - 1) * (uint32_t)p.b.row_stride;
+        b[i] = p.b.codes + min(n0 + 16 * i + col, p.N - 1) * p.b.row_stride;
         if constexpr (BYROW)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                sb_row[4 * i + r] = (uint32_t)min((int64_t)(16 * i + 4 * quarter + r), p.N - n0 - 1) * (uint32_t)p.b.scale_row_stride;
+            for (int r = 0; r < 4; ++r) sb[4 * i + r] = p.b.scale + min(n0 + 16 * i + 4 * quarter + r, p.N - 1) * p.b.scale_row_stride;
     }
-    if constexpr (!BYROW) sb_row[0] = 0;   // (16 NT rows from a multiple of 16 NT share their scale)
-    v4f acc[NT][MT] = {};
-    const int64_t steps = (p.K + kGroup - 1) / kGroup;
-    for (int64_t s0 = wave; s0 < steps; s0 += WAVES * AHEAD) {
-        v8i bv[AHEAD][NT], av[AHEAD][MT];
-        float fa[AHEAD][MT], fb[AHEAD][BYROW ? 4 * NT : 1];
+    if constexpr (!BYROW) sb[0] = p.b.scale + n0 / kGroup * p.b.scale_row_stride;   // (16 NT rows from a multiple of 16 NT share it)
+    v4f acc[NT] = {};
+    auto add = [&](const v8i (&bv)[NT], const float (&fb)[BYROW ? 4 * NT : 1], v8i av, float fa) {
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int64_t s = s0 + u * WAVES;
-            if (s < steps) {
-                const bool whole = (s + 1) * kGroup <= p.K;
+        for (int i = 0; i < NT; ++i) {
+            const v4f d = dot128<WIDE>(bv[i], av);
 #pragma unroll
-                for (int i = 0; i < NT; ++i) bv[u][i] = load_chunks(b + b_row[i], s * kGroup, p.K, quarter, whole);
-#pragma unroll
-                for (int i = 0; i < (BYROW ? 4 * NT : 1); ++i) fb[u][i] = sb[sb_row[i] + s * p.b.scale_block_stride];
-#pragma unroll
-                for (int j = 0; j < MT; ++j) {
-                    av[u][j] = load_chunks(a + a_row[j], s * kGroup, p.K, quarter, whole);
-                    fa[u][j] = sa[sa_row[j] + s * p.a.scale_block_stride];
-                }
-            }
+            for (int r = 0; r < 4; ++r) acc[i][r] += d[r] * (fa * fb[BYROW ? 4 * i + r : 0]);
         }
+    };
+    auto load = [&](int64_t s, auto REST, v8i (&bv)[NT], float (&fb)[BYROW ? 4 * NT : 1], v8i& av, float& fa) {
+        const int left = (int)min(p.K - s * kGroup, (int64_t)kGroup);
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-            if (s0 + u * WAVES < steps) {
+        for (int i = 0; i < NT; ++i) bv[i] = load_chunks<REST>(b[i] + s * kGroup, quarter, left);
 #pragma unroll
-                for (int j = 0; j < MT; ++j)
+        for (int i = 0; i < (BYROW ? 4 * NT : 1); ++i) fb[i] = sb[i][s * p.b.scale_block_stride];
+        av = v8i{0, 0, 0, 0, 0, 0, 0, 0};
+        fa = 0.f;
+        if (of_a) {
+            av = load_chunks<REST>(a + s * kGroup, quarter, left);
+            fa = sa[s * p.a.scale_block_stride];
+        }
+    };
+    const int64_t whole = p.K / kGroup;
+    for (int64_t s0 = wave; s0 < whole; s0 += WAVES * kAhead) {
+        v8i bv[kAhead][NT], av[kAhead];
+        float fb[kAhead][BYROW ? 4 * NT : 1], fa[kAhead];
 #pragma unroll
-                    for (int i = 0; i < NT; ++i) {
-                        const v4f d = dot128<WIDE>(bv[u][i], av[u][j]);
+        for (int u = 0; u < kAhead; ++u)   // (behind the end: the first block again, not added)
+            load(s0 + u * WAVES < whole ? s0 + u * WAVES : s0, Int<0>(), bv[u], fb[u], av[u], fa[u]);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[i][j][r] += d[r] * (fa[u][j] * fb[u][BYROW ? 4 * i + r : 0]);
-                    }
-            }
+        for (int u = 0; u < kAhead; ++u)
+            if (s0 + u * WAVES < whole) add(bv[u], fb[u], av[u], fa[u]);
+    }
+    if (p.K > whole * kGroup && whole % WAVES == wave) {
+        v8i bv[NT], av;
+        float fb[BYROW ? 4 * NT : 1], fa;
+        load(whole, Int<1>(), bv, fb, av, fa);
+        add(bv, fb, av, fa);
     }
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        if (i) __syncthreads();
+    for (int i = 0; i < NT; ++i) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    for (int at = threadIdx.x; at < NT * 256; at += 64 * WAVES) {
+        // rows of results first, so that a row's results lie together
+        const int m = at / (16 * NT), c = at % (16 * NT), l = m + 16 * (c >> 2 & 3);
+        if (m < p.M && n0 + c < p.N) {
+            float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[i][j];
-        __syncthreads();
-        for (int at = threadIdx.x; at < MT * 64; at += 64 * WAVES) {
-            const int j = at >> 6, l = at & 63;
-            v4f sum = sums[0][j][l];
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w) {
-                const v4f v = sums[w][j][l];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) sum[r] += v[r];
-            }
-            const int64_t m = m0 + 16 * j + (l & 15), n = n0 + 16 * i + 4 * (l >> 4);
-            if (m < p.M) {
-                E* const to = static_cast<E*>(p.out) + m * p.out_stride + n;
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (n + r < p.N) to[r] = (E)sum[r];
-            }
+            for (int w = 0; w < WAVES; ++w) sum += sums[w][c >> 4][l][c & 3];
+            static_cast<E*>(p.out)[m * p.out_stride + n0 + c] = (E)sum;
         }
     }
 }
@@ -607,14 +598,10 @@ void launch_shape(const TileParams& t, const gvr_fp8::MatmulPlan& plan, hipStrea
     auto go = [&](auto kernel, auto params) { hipLaunchKernelGGL(kernel, grid, block, 0, s, params); };
     switch (plan.shape) {
         case gvr_fp8::kAnyShape: go(matmul_kernel<E>, t.p); break;
-        case gvr_fp8::kRows16: plan.threads == 512 ? go(rows_kernel<E, BYROW, 1, 1, 4, 8>, t.p) : go(rows_kernel<E, BYROW, 1, 1, 4, 16>, t.p); break;
-        case gvr_fp8::kRows32: go(rows_kernel<E, BYROW, 2, 1, 4, 8>, t.p); break;
-        case gvr_fp8::kRows64: go(rows_kernel<E, BYROW, 4, 1, 2, 8>, t.p); break;
-        case gvr_fp8::kRows64x2: go(rows_kernel<E, BYROW, 4, 2, 2, 8>, t.p); break;
-        case gvr_fp8::kRows128: go(rows_kernel<E, BYROW, 8, 1, 2, 8>, t.p); break;
-        case gvr_fp8::kRows128x2: go(rows_kernel<E, BYROW, 8, 2, 1, 8>, t.p); break;
-        case gvr_fp8::kLow: go(tile_kernel<E, BYROW, 64, 128, 64, 32, 5>, t); break;
-        case gvr_fp8::kNarrow: go(tile_kernel<E, BYROW, 128, 64, 64, 32, 5>, t); break;
+        case gvr_fp8::kRows: plan.threads == 512 ? go(rows_kernel<E, BYROW, 1, 8>, t.p) : go(rows_kernel<E, BYROW, 1, 16>, t.p); break;
+        case gvr_fp8::kRowPairs: go(rows_kernel<E, BYROW, 2, 8>, t.p); break;
+        case gvr_fp8::kLow: go(tile_kernel<E, BYROW, 64, 128, 64, 32, 3>, t); break;
+        case gvr_fp8::kNarrow: go(tile_kernel<E, BYROW, 128, 64, 64, 32, 3>, t); break;
         case gvr_fp8::kSquare: go(tile_kernel<E, BYROW, 128, 128, 64, 64, 2>, t); break;
         case gvr_fp8::kLarge:
             if constexpr (sizeof(E) == 2) go(tile_kernel<E, BYROW, 256, 256, 128, 64, 2>, t);

@@ -92,25 +92,27 @@ inline gvr_status check_matmul(const gvr_fp8_matrix* a, const gvr_fp8_matrix* b,
 }
 
 constexpr int kTileM = 64, kTileN = 64, kThreads = 256;   // of the kernel that takes any alignment
-enum Shape { kAnyShape, kRows16, kRows32, kRows64, kRows64x2, kRows128, kRows128x2, kLow, kNarrow, kSquare, kLarge };
+enum Shape { kAnyShape, kRows, kRowPairs, kLow, kNarrow, kSquare, kLarge };
+// Rows of A and of B of a workgroup and its threads; and, measured on 256 compute
+// units over K = 4096, the microseconds of a step of 128 elements where a unit runs
+// one workgroup and where it runs two (0: it holds one), and of a workgroup's begin and end.
 struct Tiles {
-    int m, n, threads;   // rows of A and of B of a workgroup
+    int m, n, threads;
+    double one, two, ends;
 };
 inline Tiles tiles_of(Shape s) {
     switch (s) {
-        case kRows16: return {16, 16, 512};
-        case kRows32: return {32, 16, 512};
-        case kRows64: return {64, 16, 512};
-        case kRows64x2: return {64, 32, 512};
-        case kRows128: return {128, 16, 512};
-        case kRows128x2: return {128, 32, 512};
-        case kLow: return {64, 128, 256};
-        case kNarrow: return {128, 64, 256};
-        case kSquare: return {128, 128, 256};
-        case kLarge: return {256, 256, 512};
-        default: return {kTileM, kTileN, kThreads};
+        case kRows: return {16, 16, 512, 0, 0, 0};
+        case kRowPairs: return {16, 32, 512, 0, 0, 0};
+        case kLow: return {64, 128, 256, 0.60, 0.76, 3.5};
+        case kNarrow: return {128, 64, 256, 0.60, 0.76, 3.5};
+        case kSquare: return {128, 128, 256, 0.87, 1.33, 3.5};
+        case kLarge: return {256, 256, 512, 1.60, 0, 8.0};
+        default: return {kTileM, kTileN, kThreads, 0, 0, 0};
     }
 }
+constexpr int kRowsMost = 16;   // rows of A up to which the kernels without tiles serve
+constexpr int64_t kUnits = 256; // compute units
 
 struct MatmulPlan {
     Shape shape;
@@ -134,24 +136,47 @@ inline bool scale_quads(const gvr_fp8_matrix& m, int64_t K, int64_t steps_each) 
            groups_of(K) % 4 == 0 && K % kGroup == 0 && steps_each % 4 == 0;
 }
 
+// The time that a shape takes, in microseconds: rounds of workgroups, each as long
+// as its steps, and where the sum is split the kernel that joins the parts.
+inline double matmul_time(const Tiles& t, int64_t M, int64_t N, int64_t steps, int64_t splits) {
+    const int64_t units = ((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n) * splits, each = (steps + splits - 1) / splits;
+    const int64_t round = t.two > 0 ? 2 * kUnits : kUnits, whole = units / round, rest = units % round;
+    const double full = t.ends + each * (t.two > 0 ? t.two : t.one);
+    double us = whole * full + (rest == 0 ? 0 : rest <= kUnits ? t.ends + each * t.one : full);
+    if (splits > 1) us += 2.5 + 8.0e-6 * M * N * splits / 4.5;
+    return us;
+}
+
 inline gvr_status plan_matmul(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, int64_t M, int64_t N, int64_t K, bool wide,
                               size_t ws_bytes, MatmulPlan* p) {
-    const bool tiles = tile_rows(a, 256, K) && tile_rows(b, 256, K);
-    p->shape = !tiles ? kAnyShape : M <= 16 ? kRows16 : M <= 32 ? kRows32 : !wide && M * N >= (int64_t)256 * 256 * 128 ? kLarge : kSquare;
+    const int64_t steps = groups_of(K);
+    int64_t splits = 1;
+    p->shape = kAnyShape;
+    if (tile_rows(a, 256, K) && tile_rows(b, 256, K)) {
+        if (M <= kRowsMost) {
+            p->shape = N >= 32 * kUnits ? kRowPairs : kRows;
+        } else {
+            double best = 1e300;
+            for (const Shape s : {kLow, kNarrow, kSquare, kLarge})
+                for (const int64_t n : {1, 2, 3, 4, 6, 8, 12, 16}) {
+                    if (s == kLarge && wide) continue;   // (its sums are on the FP8 matrix cores)
+                    if (n > 1 && (steps < 4 * n || (double)n * M * N * 4 > (double)ws_bytes)) break;
+                    const double us = matmul_time(tiles_of(s), M, N, steps, n);
+                    if (us < best) best = us, p->shape = s, splits = n;
+                }
+        }
+    }
     const Tiles t = tiles_of(p->shape);
     p->threads = t.threads;
     p->tiles_m = (M + t.m - 1) / t.m;
     p->tiles_n = (N + t.n - 1) / t.n;   // (each at most 2^27)
-    if (p->shape == kRows16 && p->tiles_n < 256) p->threads = 1024;
-    int64_t steps = groups_of(K), splits = 1;
+    if (p->shape == kRows && p->tiles_n < kUnits) p->threads = 1024;   // (more waves where workgroups are few)
     // SWEEP
     p->steps_each = (steps + splits - 1) / splits;
-    if (splits > 1) p->steps_each = (p->steps_each + 3) / 4 * 4;
+    if (splits > 1) p->steps_each = (p->steps_each + 3) / 4 * 4;   // (scales come four at a time)
     p->splits = p->steps_each ? (steps + p->steps_each - 1) / p->steps_each : 1;
-    if (p->splits < 1) p->splits = 1;
     p->band = 8;
     p->workspace = p->splits > 1 ? (size_t)p->splits * M * N * 4 : 0;
-    if (p->workspace > ws_bytes) p->splits = 1, p->steps_each = steps, p->workspace = 0;
     p->workgroups = p->tiles_m * p->tiles_n * p->splits;
     return p->workgroups * p->threads > 0xFFFFFFFFll ? GVR_ERR_TOO_LONG : GVR_OK;
 }
