@@ -468,13 +468,18 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
     }
 }
 
-// --- up to 16 rows of A
+// --- up to 32 rows of A
 //
-// A workgroup multiplies 16 NT rows of B with all rows of A; its waves share out the
-// blocks of 128 and their sums are added at the end, in the order of the waves. Codes
-// go from memory to registers, kAhead blocks of a wave at a time, with no barrier on
-// the way. Lane l holds chunks l / 16 and l / 16 + 4 of its rows.
-constexpr int kAhead = 4;
+// A workgroup multiplies 16 NT rows of B with all rows of A (at most 16 MT); its
+// waves share out the blocks of 128 and their sums are added at the end, in the order
+// of the waves. Codes go from memory to registers, AHEAD blocks of a wave at a time,
+// with no barrier on the way; lanes whose row A does not have load nothing. Lane l
+// holds chunks l / 16 and l / 16 + 4 of its rows.
+// Bound by how fast a compute unit takes in B (1 x 8192 x 4096: 34 MB in 8.0 us =
+// 4.2 TB/s; 1 x 4096 x 4096: 5.9, of which launch and sums 3.5) and A's rows beside it
+// (16 rows: 9.7). Up to 16 rows the tile kernels take 11.7 us on 8192 rows of B, with
+// 17 and 32 rows on 4096 of them 11.2 and 11.8 against 7.9 and 9.7; on 8192 the two
+// are even at 32 rows (12.4, 12.6), with 64 rows the tiles are ahead (13.2).
 
 // Chunks `quarter` and `quarter` + 4 of a row's 128 bytes; REST: of the last ones, zeros past `left`.
 template <bool REST>
@@ -495,16 +500,21 @@ DEV v8i load_chunks(const uint8_t* row, int quarter, int left) {
     return v8i{(int)v[0][0], (int)v[0][1], (int)v[0][2], (int)v[0][3], (int)v[1][0], (int)v[1][1], (int)v[1][2], (int)v[1][3]};
 }
 
-template <class E, bool BYROW, int NT, int WAVES>
+template <class E, bool BYROW, int MT, int NT, int AHEAD, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void rows_kernel(MatmulParams p) {
     constexpr bool WIDE = sizeof(E) == 4;
-    __shared__ v4f sums[WAVES][NT][64];
+    __shared__ v4f sums[WAVES][MT][64];
     const int lane = threadIdx.x & 63, wave = (int)uniform(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
     const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
     // rows of B past the end read the last one and are not stored, those of A are zeros
-    const bool of_a = col < p.M;
-    const uint8_t* const a = p.a.codes + (of_a ? col : 0) * p.a.row_stride;
-    const float* const sa = p.a.scale + (of_a ? col : 0) * p.a.scale_row_stride;
+    const uint8_t* a[MT];
+    const float* sa[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+        const int m = 16 * j + col < p.M ? 16 * j + col : 0;
+        a[j] = p.a.codes + m * p.a.row_stride;
+        sa[j] = p.a.scale + m * p.a.scale_row_stride;
+    }
     const uint8_t* b[NT];
     const float* sb[BYROW ? 4 * NT : 1];
 #pragma unroll
@@ -515,56 +525,66 @@ __global__ __launch_bounds__(64 * WAVES) void rows_kernel(MatmulParams p) {
             for (int r = 0; r < 4; ++r) sb[4 * i + r] = p.b.scale + min(n0 + 16 * i + 4 * quarter + r, p.N - 1) * p.b.scale_row_stride;
     }
     if constexpr (!BYROW) sb[0] = p.b.scale + n0 / kGroup * p.b.scale_row_stride;   // (16 NT rows from a multiple of 16 NT share it)
-    v4f acc[NT] = {};
-    auto add = [&](const v8i (&bv)[NT], const float (&fb)[BYROW ? 4 * NT : 1], v8i av, float fa) {
+    v4f acc[NT][MT] = {};
+    auto add = [&](const v8i (&bv)[NT], const float (&fb)[BYROW ? 4 * NT : 1], const v8i (&av)[MT], const float (&fa)[MT]) {
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            const v4f d = dot128<WIDE>(bv[i], av);
+        for (int j = 0; j < MT; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[i][r] += d[r] * (fa * fb[BYROW ? 4 * i + r : 0]);
-        }
+            for (int i = 0; i < NT; ++i) {
+                const v4f d = dot128<WIDE>(bv[i], av[j]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[i][j][r] += d[r] * (fa[j] * fb[BYROW ? 4 * i + r : 0]);
+            }
     };
-    auto load = [&](int64_t s, auto REST, v8i (&bv)[NT], float (&fb)[BYROW ? 4 * NT : 1], v8i& av, float& fa) {
+    auto load = [&](int64_t s, auto REST, v8i (&bv)[NT], float (&fb)[BYROW ? 4 * NT : 1], v8i (&av)[MT], float (&fa)[MT]) {
         const int left = (int)min(p.K - s * kGroup, (int64_t)kGroup);
 #pragma unroll
         for (int i = 0; i < NT; ++i) bv[i] = load_chunks<REST>(b[i] + s * kGroup, quarter, left);
 #pragma unroll
         for (int i = 0; i < (BYROW ? 4 * NT : 1); ++i) fb[i] = sb[i][s * p.b.scale_block_stride];
-        av = v8i{0, 0, 0, 0, 0, 0, 0, 0};
-        fa = 0.f;
-        if (of_a) {
-            av = load_chunks<REST>(a + s * kGroup, quarter, left);
-            fa = sa[s * p.a.scale_block_stride];
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+            av[j] = v8i{0, 0, 0, 0, 0, 0, 0, 0};
+            fa[j] = 0.f;
+            if (16 * j + col < p.M) {
+                av[j] = load_chunks<REST>(a[j] + s * kGroup, quarter, left);
+                fa[j] = sa[j][s * p.a.scale_block_stride];
+            }
         }
     };
     const int64_t whole = p.K / kGroup;
-    for (int64_t s0 = wave; s0 < whole; s0 += WAVES * kAhead) {
-        v8i bv[kAhead][NT], av[kAhead];
-        float fb[kAhead][BYROW ? 4 * NT : 1], fa[kAhead];
+    for (int64_t s0 = wave; s0 < whole; s0 += WAVES * AHEAD) {
+        v8i bv[AHEAD][NT], av[AHEAD][MT];
+        float fb[AHEAD][BYROW ? 4 * NT : 1], fa[AHEAD][MT];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)   // (behind the end: the first block again, not added)
+        for (int u = 0; u < AHEAD; ++u)   // (behind the end: the first block again, not added)
             load(s0 + u * WAVES < whole ? s0 + u * WAVES : s0, Int<0>(), bv[u], fb[u], av[u], fa[u]);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
+        for (int u = 0; u < AHEAD; ++u)
             if (s0 + u * WAVES < whole) add(bv[u], fb[u], av[u], fa[u]);
     }
     if (p.K > whole * kGroup && whole % WAVES == wave) {
-        v8i bv[NT], av;
-        float fb[BYROW ? 4 * NT : 1], fa;
+        v8i bv[NT], av[MT];
+        float fb[BYROW ? 4 * NT : 1], fa[MT];
         load(whole, Int<1>(), bv, fb, av, fa);
         add(bv, fb, av, fa);
     }
 #pragma unroll
-    for (int i = 0; i < NT; ++i) sums[wave][i][lane] = acc[i];
-    __syncthreads();
-    for (int at = threadIdx.x; at < NT * 256; at += 64 * WAVES) {
-        // rows of results first, so that a row's results lie together
-        const int m = at / (16 * NT), c = at % (16 * NT), l = m + 16 * (c >> 2 & 3);
-        if (m < p.M && n0 + c < p.N) {
-            float sum = 0.f;
+    for (int i = 0; i < NT; ++i) {
+        if (i) __syncthreads();
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) sum += sums[w][c >> 4][l][c & 3];
-            static_cast<E*>(p.out)[m * p.out_stride + n0 + c] = (E)sum;
+        for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[i][j];
+        __syncthreads();
+        for (int at = threadIdx.x; at < MT * 256; at += 64 * WAVES) {
+            // rows of results first, so that a row's results lie together
+            const int m = at / 16, c = at % 16, l = m % 16 + 16 * (c >> 2);
+            const int64_t n = n0 + 16 * i + c;
+            if (m < p.M && n < p.N) {
+                float sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) sum += sums[w][m >> 4][l][c & 3];
+                static_cast<E*>(p.out)[m * p.out_stride + n] = (E)sum;
+            }
         }
     }
 }
@@ -598,8 +618,9 @@ void launch_shape(const TileParams& t, const gvr_fp8::MatmulPlan& plan, hipStrea
     auto go = [&](auto kernel, auto params) { hipLaunchKernelGGL(kernel, grid, block, 0, s, params); };
     switch (plan.shape) {
         case gvr_fp8::kAnyShape: go(matmul_kernel<E>, t.p); break;
-        case gvr_fp8::kRows: plan.threads == 512 ? go(rows_kernel<E, BYROW, 1, 8>, t.p) : go(rows_kernel<E, BYROW, 1, 16>, t.p); break;
-        case gvr_fp8::kRowPairs: go(rows_kernel<E, BYROW, 2, 8>, t.p); break;
+        case gvr_fp8::kRows: plan.threads == 512 ? go(rows_kernel<E, BYROW, 1, 1, 4, 8>, t.p) : go(rows_kernel<E, BYROW, 1, 1, 4, 16>, t.p); break;
+        case gvr_fp8::kRowPairs: go(rows_kernel<E, BYROW, 1, 2, 4, 8>, t.p); break;
+        case gvr_fp8::kRows32: go(rows_kernel<E, BYROW, 2, 1, 4, 8>, t.p); break;
         case gvr_fp8::kLow: go(tile_kernel<E, BYROW, 64, 128, 64, 32, 3>, t); break;
         case gvr_fp8::kNarrow: go(tile_kernel<E, BYROW, 128, 64, 64, 32, 3>, t); break;
         case gvr_fp8::kSquare: go(tile_kernel<E, BYROW, 128, 128, 64, 64, 2>, t); break;

@@ -92,7 +92,7 @@ inline gvr_status check_matmul(const gvr_fp8_matrix* a, const gvr_fp8_matrix* b,
 }
 
 constexpr int kTileM = 64, kTileN = 64, kThreads = 256;   // of the kernel that takes any alignment
-enum Shape { kAnyShape, kRows, kRowPairs, kLow, kNarrow, kSquare, kLarge };
+enum Shape { kAnyShape, kRows, kRowPairs, kRows32, kLow, kNarrow, kSquare, kLarge };
 // Rows of A and of B of a workgroup and its threads; and, measured on 256 compute
 // units over K = 4096, the microseconds of a step of 128 elements where a unit runs
 // one workgroup and where it runs two (0: it holds one), and of a workgroup's begin and end.
@@ -104,6 +104,7 @@ inline Tiles tiles_of(Shape s) {
     switch (s) {
         case kRows: return {16, 16, 512, 0, 0, 0};
         case kRowPairs: return {16, 32, 512, 0, 0, 0};
+        case kRows32: return {32, 16, 512, 0, 0, 0};
         case kLow: return {64, 128, 256, 0.60, 0.76, 3.5};
         case kNarrow: return {128, 64, 256, 0.60, 0.76, 3.5};
         case kSquare: return {128, 128, 256, 0.87, 1.33, 3.5};
@@ -111,7 +112,6 @@ inline Tiles tiles_of(Shape s) {
         default: return {kTileM, kTileN, kThreads, 0, 0, 0};
     }
 }
-constexpr int kRowsMost = 16;   // rows of A up to which the kernels without tiles serve
 constexpr int64_t kUnits = 256; // compute units
 
 struct MatmulPlan {
@@ -153,8 +153,12 @@ inline gvr_status plan_matmul(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, 
     int64_t splits = 1;
     p->shape = kAnyShape;
     if (tile_rows(a, 256, K) && tile_rows(b, 256, K)) {
-        if (M <= kRowsMost) {
+        // Few rows of A: the kernels without tiles (the times are at them), with two tiles of B's rows to a workgroup
+        // where that still gives one to each compute unit (1 x 8192 x 4096: 8.0 us, with one 8.6; 16 x: 9.7, 11.7).
+        if (M <= 16) {
             p->shape = N >= 32 * kUnits ? kRowPairs : kRows;
+        } else if (M <= 32 && N <= 16 * kUnits) {
+            p->shape = kRows32;
         } else {
             double best = 1e300;
             for (const Shape s : {kLow, kNarrow, kSquare, kLarge})
