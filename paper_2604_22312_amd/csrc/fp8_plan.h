@@ -20,7 +20,23 @@ constexpr int kMaxHead = 1 << 20; // elements of a head, and heads
 
 inline int64_t groups_of(int64_t n) { return (n + kGroup - 1) / kGroup; }
 
-// --- heads: 16 lanes take a block of 128 elements, eight each
+// Division of 32-bit numbers below 2^31 by a number that the launch knows: n / d is
+// the upper half of n * mul, shifted (mul = ceil(2^(32 + shift) / d), shift the bits of
+// d - 1, fits 33 bits; its upper bit is added by hand).
+struct Divisor {
+    uint32_t d, mul, shift;
+};
+inline Divisor divisor(uint32_t d) {
+    Divisor r = {d, 0, 0};
+    while (((uint64_t)1 << r.shift) < d) ++r.shift;
+    r.mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << r.shift) - d)) / d + 1);
+    return r;
+}
+inline uint32_t quotient(uint32_t n, const Divisor& r) {
+    return (uint32_t)((((uint64_t)n * r.mul >> 32) + n) >> r.shift);
+}
+
+// --- heads: a thread takes 8 elements of a block of 128, or 16
 struct HeadsPlan {
     int64_t tokens, blocks, rows;   // of a launch row (blockIdx.y), workgroups in x, launch rows
 };

@@ -1,8 +1,8 @@
 // fp8_quantize.hip -- E4M3 codes and a scale per 128 elements, of heads and of
 // matrices in both directions, behind include/gvr_fp8.h.
 //
-// Heads: a thread takes eight elements, the 16 lanes of a row a block of 128, so
-// the block's largest magnitude is four lane exchanges.
+// Heads: a thread takes eight elements (or sixteen), so the largest magnitude of a
+// block of 128 is four (three) lane exchanges.
 //
 // Matrices: a workgroup takes 128 x 128 elements, a thread eight columns of eight
 // rows, held in registers between the search for the largest magnitudes and the
@@ -19,7 +19,9 @@
 #include "gvr_fp8.h"
 #include "elem_ops.h"
 #include "fp8_codes.h"
+#pragma clang force_cuda_host_device begin
 #include "fp8_plan.h"
+#pragma clang force_cuda_host_device end
 
 namespace {
 
@@ -37,21 +39,22 @@ struct HeadsParams {
     float* scale;
     int64_t xt, xh, ct, ch, st, sh;   // strides in elements
     int64_t n_pos, T, tokens, rows;
-    int32_t H, D, rot, groups;
+    int32_t D, rot;
+    gvr_fp8::Divisor per_token, per_head;   // threads
     bool inter, pow2;
 };
 
-enum { kNoTurn, kHalf, kInter, kAny };   // rotations; kAny also serves rows of any alignment and length
+enum { kNoTurn, kHalf, kInter, kAny, kNoTurn16 };   // rotations; kAny also serves rows of any alignment and length
 
-template <class E, int MODE>
+template <class E, int MODE, int PER>
 __global__ __launch_bounds__(kBlock) void heads_kernel(HeadsParams p) {
     constexpr bool WIDE = MODE != kAny;
+    constexpr int LANES = kGroup / PER;   // of a block
     const uint32_t idx = blockIdx.x * (uint32_t)kBlock + threadIdx.x;
-    const uint32_t per_head = (uint32_t)p.groups * 16, per = (uint32_t)p.H * per_head;
-    const uint32_t tt = idx / per, r = idx - tt * per;
-    const int h = (int)(r / per_head), e = 8 * (int)(r - (uint32_t)h * per_head);
+    const uint32_t tt = gvr_fp8::quotient(idx, p.per_token), r = idx - tt * p.per_token.d;
+    const int h = (int)gvr_fp8::quotient(r, p.per_head), e = PER * (int)(r - (uint32_t)h * p.per_head.d);
     const int64_t t = (int64_t)blockIdx.y * p.tokens + tt;
-    if ((int64_t)tt >= p.tokens || t >= p.T) return;   // (all 16 lanes of a block)
+    if ((int64_t)tt >= p.tokens || t >= p.T) return;   // (all lanes of a block)
     int64_t row = t;
     if (p.slots) {
         row = p.slots[t];
@@ -65,9 +68,10 @@ __global__ __launch_bounds__(kBlock) void heads_kernel(HeadsParams p) {
         const int32_t pos = p.positions[t];
         if (pos >= 0 && pos < p.n_pos) cs = p.cs + (int64_t)pos * p.rot;
     }
-    f8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+    f8 v = {0, 0, 0, 0, 0, 0, 0, 0}, w = v;
     if constexpr (WIDE) {
         if (left > 0) v = load8<true>(x + e);
+        if (PER == 16 && left > 8) w = load8<true>(x + e + 8);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -106,17 +110,21 @@ __global__ __launch_bounds__(kBlock) void heads_kernel(HeadsParams p) {
             }
         }
     }
-    const Scale sc = scale_of(row_largest(largest(v)), p.pow2);
+    const Scale sc = scale_of(row_largest<LANES>(max(largest(v), largest(w))), p.pow2);
     const uint2 codes = codes_of(v, sc);
     uint8_t* const out = p.codes + row * p.ct + h * p.ch + e;
-    if constexpr (WIDE) {
+    if constexpr (PER == 16) {
+        const uint2 more = codes_of(w, sc);
+        if (left >= 16) *reinterpret_cast<uint4*>(out) = uint4{codes.x, codes.y, more.x, more.y};
+        else if (left > 0) *reinterpret_cast<uint2*>(out) = codes;
+    } else if constexpr (WIDE) {
         if (left > 0) *reinterpret_cast<uint2*>(out) = codes;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < left) out[i] = (uint8_t)((i < 4 ? codes.x : codes.y) >> (8 * (i & 3)));
     }
-    if ((threadIdx.x & 15) == 0) p.scale[row * p.st + h * p.sh + e / kGroup] = sc.scale;
+    if ((threadIdx.x & (LANES - 1)) == 0) p.scale[row * p.st + h * p.sh + e / kGroup] = sc.scale;
 }
 
 template <class E>
@@ -124,9 +132,10 @@ gvr_status launch_heads(const HeadsParams& p, const gvr_fp8::HeadsPlan& l, int m
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)l.blocks, (unsigned)l.rows), dim3(kBlock), 0, (hipStream_t)stream, p);
     };
-    mode == kNoTurn ? go(heads_kernel<E, kNoTurn>)
-    : mode == kHalf ? go(heads_kernel<E, kHalf>)
-    : mode == kInter ? go(heads_kernel<E, kInter>) : go(heads_kernel<E, kAny>);
+    mode == kNoTurn16 ? go(heads_kernel<E, kNoTurn, 16>)
+    : mode == kNoTurn ? go(heads_kernel<E, kNoTurn, 8>)
+    : mode == kHalf ? go(heads_kernel<E, kHalf, 8>)
+    : mode == kInter ? go(heads_kernel<E, kInter, 8>) : go(heads_kernel<E, kAny, 8>);
     return hipGetLastError() == hipSuccess ? GVR_OK : GVR_ERR_HIP;
 }
 
@@ -197,7 +206,7 @@ __global__ __launch_bounds__(kBlock) void matrix_kernel(MatrixParams p) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int64_t r = r0 + 8 * tr + i;
-            const Scale s = p.square ? whole : scale_of(row_largest(largest(v[i])), p.pow2);
+            const Scale s = p.square ? whole : scale_of(row_largest<16>(largest(v[i])), p.pow2);
             straight[i] = codes_of(v[i], s);
             if (p.out.codes && r < p.R) {
                 const uint32_t w[2] = {straight[i].x, straight[i].y};
@@ -288,13 +297,10 @@ gvr_status gvr_fp8_quantize(const gvr_heads* x, int32_t dtype, int64_t T, int32_
     p.xt = x->token_stride, p.xh = x->head_stride;
     p.ct = out->token_stride, p.ch = out->head_stride;
     p.st = out->scale_token_stride, p.sh = out->scale_head_stride;
-    p.T = T, p.rows = rows, p.H = H, p.D = D;
-    p.groups = (int32_t)gvr_fp8::groups_of(D);
+    p.T = T, p.rows = rows, p.D = D;
     p.cs = cs ? cs->data : nullptr, p.n_pos = cs ? cs->positions : 0, p.rot = cs ? cs->rot : 0;
     p.inter = cs && (cs->flags & GVR_ROPE_INTERLEAVED);
     p.pow2 = flags & GVR_FP8_POW2;
-    const gvr_fp8::HeadsPlan l = gvr_fp8::plan_heads(T, (int64_t)H * p.groups * 16);
-    p.tokens = l.tokens;
     const int size = gvr_rot::dtype_size(dtype);
     const bool wide = gvr_rot::wide_rows(*x, size) && D % 8 == 0 && ((uintptr_t)p.codes & 7) == 0 && p.ct % 8 == 0 &&
                       p.ch % 8 == 0;
@@ -307,6 +313,16 @@ gvr_status gvr_fp8_quantize(const gvr_heads* x, int32_t dtype, int64_t T, int32_
         else
             mode = p.rot % 16 == 0 ? kHalf : kAny;
     }
+    const int64_t blocks = (int64_t)H * gvr_fp8::groups_of(D);
+    // Sixteen elements a thread where that leaves threads enough to fill the device.
+    if (mode == kNoTurn && ((uintptr_t)p.codes & 15) == 0 && p.ct % 16 == 0 && p.ch % 16 == 0 &&
+        T * blocks >= (int64_t)256 * 2048 / 8)
+        mode = kNoTurn16;
+    const int64_t lanes = mode == kNoTurn16 ? 8 : 16;   // threads of a block
+    const gvr_fp8::HeadsPlan l = gvr_fp8::plan_heads(T, blocks * lanes);
+    p.tokens = l.tokens;
+    p.per_token = gvr_fp8::divisor((uint32_t)(blocks * lanes));
+    p.per_head = gvr_fp8::divisor((uint32_t)(gvr_fp8::groups_of(D) * lanes));
     return dtype == GVR_BF16 ? launch_heads<__bf16>(p, l, mode, stream)
            : dtype == GVR_F16 ? launch_heads<_Float16>(p, l, mode, stream)
                               : launch_heads<float>(p, l, mode, stream);
