@@ -4,6 +4,7 @@
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import NamedTuple
 
 import torch
@@ -234,6 +235,54 @@ def gvr_fp8_matmul(a, a_scale, b, b_scale, out=None, dtype=torch.bfloat16, works
     return prepare_gvr_fp8_matmul(a, a_scale, b, b_scale, out, dtype, workspace, stream)()
 
 
+# gvr_fp8_linear makes its matrices in two blocks of memory, one for the call and one
+# that the backward pass keeps, and hands the library pointers into them: six calls
+# with tensors of their own and their checks took 340 us of host time a step.
+
+class _Block:
+    """Places of matrices in one block of memory that is allocated when all are known."""
+    __slots__ = ("size", "made")
+
+    def __init__(self):
+        self.size, self.made = 0, []
+
+    def matrix(self, rows, cols, per):
+        """An ``_Fp8Matrix`` whose pointers count from the block's start until ``place``."""
+        wide, blocks = (cols + 15) // 16 * 16, (cols + BLOCK - 1) // BLOCK
+        scale = self.size + (rows * wide + 255) // 256 * 256
+        m = _Fp8Matrix(self.size, wide, scale, blocks, 1, per, 0)
+        self.size = scale + ((rows + per - 1) // per * blocks * 4 + 255) // 256 * 256
+        self.made.append(m)
+        return m
+
+    def place(self, dev, more=0):
+        """The block, with `more` bytes behind its matrices (their address: second)."""
+        t = torch.empty(max(self.size + more, 1), dtype=torch.uint8, device=dev)
+        start = t.data_ptr()
+        for m in self.made:
+            m.codes, m.scale = start + (m.codes or 0), start + (m.scale or 0)
+        return t, start + self.size
+
+
+def _check(name, status):
+    if status != 0:
+        raise GvrError(name, status)
+
+
+@functools.lru_cache(maxsize=4096)
+def _product_workspace(M, N, K, per, device):
+    """Bytes for split sums of a product of matrices as a ``_Block`` has them (their sizes alone decide)."""
+    b = _Block()
+    sa, sb = b.matrix(M, K, 1), b.matrix(N, K, per)
+    return _matmul_workspace(sa, sb, M, N, K, torch.device("cuda", device))
+
+
+def _rows_of(x):
+    """x [...][C] as a matrix whose rows are contiguous."""
+    m = x.reshape(-1, x.shape[-1])
+    return m.contiguous() if m.shape[1] > 1 and m.stride(1) != 1 else m
+
+
 class _Linear(torch.autograd.Function):
     """y = Q(x) Q(W)^T, dx = Q(dy) Q(W), dW = Q(dy^T) Q(x^T)^T: the rounding to 8 bits
     counts as the identity. Codes of x^T and W^T are what the backward pass keeps."""
@@ -241,45 +290,81 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, codes, scale, codes_t, scale_t):
         need_x, need_w = ctx.needs_input_grad[:2]
-        x2 = x.reshape(-1, x.shape[-1])
-        if x2.shape[1] > 1 and x2.stride(1) != 1:
-            x2 = x2.contiguous()
-        xt = None
-        if need_w:
-            xq, xt = gvr_fp8_quantize_matrix(x2, transposed=True)
-        else:
-            xq = gvr_fp8_quantize(x2)
-        wq, wt = Fp8Matrix(codes, scale), Fp8Matrix(codes_t, scale_t)
+        L, dev = lib(), x.device
+        x2 = _rows_of(x)
+        (M, K), N = x2.shape, (weight if weight is not None else codes).shape[0]
+        y = torch.empty((M, N), dtype=x.dtype, device=dev)
+        now, kept = _Block(), _Block()
+        xq = now.matrix(M, K, 1)
+        xt = kept.matrix(K, M, 1) if need_w else None
         if weight is not None:
-            w2 = weight if weight.shape[1] <= 1 or weight.stride(1) == 1 else weight.contiguous()
-            wq = gvr_fp8_quantize_matrix(w2, square=True, transposed=need_x)
-            if need_x:
-                wq, wt = wq
-        ctx.save_for_backward(*(wt if need_x else (None, None)), *(xt if need_w else (None, None)))
+            wq, wt = now.matrix(N, K, BLOCK), kept.matrix(K, N, BLOCK) if need_x else None
+        else:
+            wq, wt = _matrix_struct((codes, scale), "weight", N, K, BLOCK, dev), None
+        ws = _product_workspace(M, N, K, BLOCK, dev.index)
+        block, ws_at = now.place(dev, ws)
+        saved = kept.place(dev)[0] if kept.size else None
+        with _on_device(dev):
+            stream = _stream(None, dev)
+            if need_w:
+                _check("gvr_fp8_quantize_matrix", L.gvr_fp8_quantize_matrix(
+                    x2.data_ptr(), x2.stride(0), DTYPES[x.dtype], M, K, ctypes.byref(xq), ctypes.byref(xt), 0, stream))
+            else:
+                _check("gvr_fp8_quantize", L.gvr_fp8_quantize(
+                    ctypes.byref(_Heads(x2.data_ptr(), x2.stride(0), 0)), DTYPES[x.dtype], M, 1, K, None, None,
+                    ctypes.byref(_Fp8Heads(xq.codes, xq.row_stride, 0, xq.scale, xq.scale_row_stride, 0)), None, M, 0, stream))
+            if weight is not None:
+                w2 = _rows_of(weight)
+                _check("gvr_fp8_quantize_matrix", L.gvr_fp8_quantize_matrix(
+                    w2.data_ptr(), w2.stride(0), DTYPES[weight.dtype], N, K, ctypes.byref(wq),
+                    ctypes.byref(wt) if need_x else None, FP8_SQUARE, stream))
+            _check("gvr_fp8_matmul", L.gvr_fp8_matmul(
+                ctypes.byref(xq), ctypes.byref(wq), M, N, K, y.data_ptr(), N, DTYPES[x.dtype],
+                ws_at if ws else None, ws, stream))
+        ctx.save_for_backward(saved, codes_t, scale_t)
+        ctx.sizes = M, N, K
         ctx.types = x.dtype, weight.dtype if weight is not None else None
         ctx.shape = x.shape
-        y = gvr_fp8_matmul(*xq, *wq, dtype=x.dtype)
-        return y.view(x.shape[:-1] + (y.shape[1],))
+        return y.view(x.shape[:-1] + (N,))
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        codes_t, scale_t, xt_codes, xt_scale = ctx.saved_tensors
+        saved, codes_t, scale_t = ctx.saved_tensors
         need_x, need_w = ctx.needs_input_grad[:2]
-        d = dy.reshape(-1, dy.shape[-1])
-        if d.shape[1] > 1 and d.stride(1) != 1:
-            d = d.contiguous()
-        dx = dw = dq = dt = None
-        if need_w:
-            dq = gvr_fp8_quantize_matrix(d, straight=need_x, transposed=True)
-            dq, dt = dq if need_x else (None, dq)
-        elif need_x:
-            dq = gvr_fp8_quantize(d)
-        if need_x:
-            dx = gvr_fp8_matmul(*dq, codes_t, scale_t, dtype=ctx.types[0]).view(ctx.shape)
-        if need_w:
-            dw = gvr_fp8_matmul(*dt, xt_codes, xt_scale, dtype=ctx.types[1])
-        return dx, dw, None, None, None, None
+        if not need_x and not need_w:
+            return (None,) * 6
+        (M, N, K), L, dev = ctx.sizes, lib(), dy.device
+        d = _rows_of(dy)
+        kept, now = _Block(), _Block()   # (the places that forward gave out)
+        xt = kept.matrix(K, M, 1) if need_w else None
+        if codes_t is not None:
+            wt = _matrix_struct((codes_t, scale_t), "weight_t", K, N, BLOCK, dev)
+        else:
+            wt = kept.matrix(K, N, BLOCK) if need_x else None
+        for m in kept.made:
+            m.codes, m.scale = saved.data_ptr() + (m.codes or 0), saved.data_ptr() + (m.scale or 0)
+        dq, dt = now.matrix(M, N, 1) if need_x else None, now.matrix(N, M, 1) if need_w else None
+        dx = torch.empty((M, K), dtype=ctx.types[0], device=dev) if need_x else None
+        dw = torch.empty((N, K), dtype=ctx.types[1], device=dev) if need_w else None
+        ws_x = _product_workspace(M, K, N, BLOCK, dev.index) if need_x else 0
+        ws_w = _product_workspace(N, K, M, 1, dev.index) if need_w else 0
+        ws = max(ws_x, ws_w)   # (one after the other)
+        block, ws_at = now.place(dev, ws)
+        with _on_device(dev):
+            stream = _stream(None, dev)
+            _check("gvr_fp8_quantize_matrix", L.gvr_fp8_quantize_matrix(
+                d.data_ptr(), d.stride(0), DTYPES[d.dtype], M, N, ctypes.byref(dq) if need_x else None,
+                ctypes.byref(dt) if need_w else None, 0, stream))
+            if need_x:
+                _check("gvr_fp8_matmul", L.gvr_fp8_matmul(
+                    ctypes.byref(dq), ctypes.byref(wt), M, K, N, dx.data_ptr(), K, DTYPES[dx.dtype],
+                    ws_at if ws_x else None, ws_x, stream))
+            if need_w:
+                _check("gvr_fp8_matmul", L.gvr_fp8_matmul(
+                    ctypes.byref(dt), ctypes.byref(xt), N, K, M, dw.data_ptr(), K, DTYPES[dw.dtype],
+                    ws_at if ws_w else None, ws_w, stream))
+        return dx.view(ctx.shape) if need_x else None, dw, None, None, None, None
 
 
 def gvr_fp8_linear(x, weight, weight_t=None):
