@@ -100,11 +100,16 @@ DEV uint2 codes_of(f8 x, const Scale& s) {
     uint2 c = convert8(y);
     const uint2 d = convert8(z);
     if (c.x != d.x || c.y != d.y) {
-        uint32_t r[2] = {0, 0};
+        // (element by element: few of them are beside a border in any lane)
+        const uint32_t off[2] = {c.x ^ d.x, c.y ^ d.y};
+        uint32_t r[2] = {c.x, c.y};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t at = 8 * (i & 3), lower = (i < 4 ? c.x : c.y) >> at & 0xFFu, upper = (i < 4 ? d.x : d.y) >> at & 0xFFu;
-            r[i / 4] |= (lower == upper ? lower : (lower & 0x80u) | settle(lower & 0x7Fu, x[i], s.full)) << at;
+            const uint32_t at = 8 * (i & 3);
+            if (off[i / 4] >> at & 0xFFu) {
+                const uint32_t low = r[i / 4] >> at & 0x7Fu;
+                r[i / 4] += (settle(low, x[i], s.full) - low) << at;
+            }
         }
         c.x = r[0], c.y = r[1];
     }

@@ -18,6 +18,7 @@
 
 #include "gvr_pages.h"
 #include "pages_plan.h"
+#include "wave_ops.h"
 
 #ifndef DEV
 #define DEV __device__ __forceinline__
@@ -51,14 +52,25 @@ DEV Hand hand_over(int32_t* at, int R) {
     return h;
 }
 
+// Sum of v over the lanes up to this one, by lane moves.
+template <int CTRL, int ROWS>
+DEV int64_t moved(int64_t v) {
+    const uint32_t lo = (uint32_t)gvr_dev::dpp_i<CTRL, ROWS>(0, (int)(uint32_t)v);
+    return (int64_t)((uint64_t)(uint32_t)gvr_dev::dpp_i<CTRL, ROWS>(0, (int)(v >> 32)) << 32 | lo);
+}
+DEV int64_t wave_scan(int64_t v) {
+    v += moved<gvr_dev::kRowShr1, 0xF>(v);
+    v += moved<gvr_dev::kRowShr1 + 1, 0xF>(v);
+    v += moved<gvr_dev::kRowShr1 + 3, 0xF>(v);
+    v += moved<gvr_dev::kRowShr1 + 7, 0xF>(v);
+    v += moved<gvr_dev::kRowBcast15, 0xA>(v);
+    return v + moved<gvr_dev::kRowBcast31, 0xC>(v);
+}
+
 // Sum of v over the threads up to this one; *all: over all of them. Every thread calls it.
 DEV int64_t block_scan(int64_t v, int64_t* lds, int64_t* all) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t u = __shfl_up(v, d, 64);
-        if (lane >= d) v += u;
-    }
+    v = wave_scan(v);
     __syncthreads();   // (the last scan's numbers are read)
     if (lane == 63) lds[wave] = v;
     __syncthreads();
@@ -134,34 +146,48 @@ DEV int first_above(const int32_t* v, int n, int32_t x) {
     return lo;
 }
 
+// Places `first`, `first` + step, ... of the stack from its new end up to its old one or its next one, four at a time: all
+// loads of the four before their stores (no two places share a number that they read and write).
 DEV void move_pages(const StepParams& p, const Hand& h, int64_t first, int64_t step) {
     const int R = p.pool.requests;
-    const int64_t taken = h.total[0], given = h.total[1], base = h.total[2] - taken;
-    for (int64_t q = first; q < max(taken, given); q += step) {
-        const int64_t at = base + q;   // of the stack
-        if (q < taken) {
-            const int32_t i = (int32_t)(taken - 1 - q), page = p.pool.free_pages[at];
-            const int r = first_above(h.takes, R, i);
-            const int32_t j = i - (r ? h.takes[r - 1] : 0);
-            p.pool.block_table[r * p.pool.width + h.held[r] + j] = page;
-        }
-        if (q < given && at < p.pool.pages) {
+    const int64_t taken = h.total[0], given = h.total[1], base = h.total[2] - taken, places = max(taken, given);
+    for (int64_t q0 = first; q0 < places; q0 += 4 * step) {
+        int32_t got[4], back[4];
+        int32_t *to[4], *from[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t q = q0 + u * step, at = base + q;   // of the stack
+            to[u] = from[u] = nullptr;
+            if (q < taken) {
+                const int32_t i = (int32_t)(taken - 1 - q);
+                const int r = first_above(h.takes, R, i);
+                to[u] = p.pool.block_table + r * p.pool.width + h.held[r] + (i - (r ? h.takes[r - 1] : 0));
+                got[u] = p.pool.free_pages[at];
+            }
             const int64_t k = given - 1 - q;
-            if (k >= INT32_MAX) continue;
-            const int r = first_above(h.gives, R, (int32_t)k);
-            const int32_t j = (int32_t)k - (r ? h.gives[r - 1] : 0);
-            int32_t* const entry = p.pool.block_table + r * p.pool.width + pages_of(p, h.after[r]) + j;
-            p.pool.free_pages[at] = *entry;
-            *entry = -1;
+            if (q < given && at < p.pool.pages && k < INT32_MAX) {
+                const int r = first_above(h.gives, R, (int32_t)k);
+                from[u] = p.pool.block_table + r * p.pool.width + pages_of(p, h.after[r]) + ((int32_t)k - (r ? h.gives[r - 1] : 0));
+                back[u] = *from[u];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (to[u]) *to[u] = got[u];
+            if (from[u]) {
+                p.pool.free_pages[base + q0 + u * step] = back[u];
+                *from[u] = -1;
+            }
         }
     }
 }
 
-DEV void fill_row(const StepParams& p, const Hand& h, int64_t t) {
+// starts: h.start + 1, or a copy of it.
+DEV void fill_row(const StepParams& p, const Hand& h, const int32_t* starts, int64_t t) {
     const int R = p.pool.requests;
     int32_t pos = 0, see = 0;
     int64_t slot = -1, dense = -1;
-    const int r = first_above(h.start + 1, R, (int32_t)t);
+    const int r = first_above(starts, R, (int32_t)t);
     const int32_t keep = r < R ? h.base[r] : -1;
     if (keep >= 0) {
         pos = keep + (int32_t)(t - h.start[r]);
@@ -187,7 +213,7 @@ __global__ __launch_bounds__(kThreads) void small_step_kernel(StepParams p) {
     __syncthreads();
     move_pages(p, h, threadIdx.x, blockDim.x);
     __syncthreads();
-    for (int64_t t = threadIdx.x; t < p.a.T; t += blockDim.x) fill_row(p, h, t);
+    for (int64_t t = threadIdx.x; t < p.a.T; t += blockDim.x) fill_row(p, h, h.start + 1, t);
 }
 
 __global__ __launch_bounds__(kThreads) void add_up_kernel(StepParams p) {
@@ -200,9 +226,19 @@ __global__ __launch_bounds__(kTokenThreads) void move_pages_kernel(StepParams p)
                (int64_t)gridDim.x * kTokenThreads);
 }
 
+// The row starts are searched in LDS where they fit: nine loads one after the other from L2 cost 2 us.
 __global__ __launch_bounds__(kTokenThreads) void fill_rows_kernel(StepParams p) {
+    constexpr int kMost = 2048;
+    __shared__ int32_t starts[kMost];
+    const int R = p.pool.requests;
+    const Hand h = hand_over(p.ws, R);
     const int64_t t = (int64_t)blockIdx.x * kTokenThreads + threadIdx.x;
-    if (t < p.a.T) fill_row(p, hand_over(p.ws, p.pool.requests), t);
+    const bool here = R <= kMost;
+    if (here) {
+        for (int r = threadIdx.x; r < R; r += kTokenThreads) starts[r] = h.start[1 + r];
+        __syncthreads();
+    }
+    if (t < p.a.T) fill_row(p, h, here ? starts : h.start + 1, t);
 }
 
 }  // namespace
@@ -228,7 +264,7 @@ gvr_status gvr_page_step(const gvr_page_pool* pool, const gvr_page_step_args* ar
     } else {
         hipLaunchKernelGGL(add_up_kernel, dim3(1), dim3(kThreads), 0, s, p);
         const int64_t items = args->T / pool->page_size + pool->requests;   // (pages taken at most; those given back loop)
-        const unsigned blocks = (unsigned)(items / kTokenThreads + 1 > 512 ? 512 : items / kTokenThreads + 1);
+        const unsigned blocks = (unsigned)(items / (2 * kTokenThreads) + 1 > 512 ? 512 : items / (2 * kTokenThreads) + 1);
         if (pool->requests) hipLaunchKernelGGL(move_pages_kernel, dim3(blocks), dim3(kTokenThreads), 0, s, p);
         if (args->T)
             hipLaunchKernelGGL(fill_rows_kernel, dim3((unsigned)((args->T + kTokenThreads - 1) / kTokenThreads)),
