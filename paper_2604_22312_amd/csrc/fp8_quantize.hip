@@ -111,10 +111,11 @@ __global__ __launch_bounds__(kBlock) void heads_kernel(HeadsParams p) {
         }
     }
     const Scale sc = scale_of(row_largest<LANES>(max(largest(v), largest(w))), p.pow2);
-    const uint2 codes = codes_of(v, sc);
+    constexpr bool SHORT = sizeof(E) == 2 && MODE == kNoTurn;   // (a rotated element has 32 bits)
+    const uint2 codes = codes_of<SHORT>(v, sc);
     uint8_t* const out = p.codes + row * p.ct + h * p.ch + e;
     if constexpr (PER == 16) {
-        const uint2 more = codes_of(w, sc);
+        const uint2 more = codes_of<SHORT>(w, sc);
         if (left >= 16) *reinterpret_cast<uint4*>(out) = uint4{codes.x, codes.y, more.x, more.y};
         else if (left > 0) *reinterpret_cast<uint2*>(out) = codes;
     } else if constexpr (WIDE) {
@@ -144,7 +145,7 @@ struct MatrixParams {
     int64_t stride, R, C;
     gvr_fp8_matrix out, turned;   // codes NULL: not wanted
     uint32_t col_tiles;
-    bool pow2, square;
+    bool pow2, square, wide_out;   // rows of `out` are 16-byte aligned
 };
 
 constexpr int kTurnStride = 144;   // bytes of a column's codes in LDS
@@ -164,6 +165,7 @@ DEV void put_bytes(uint8_t* to, const uint32_t (&v)[N / 4], int64_t n) {
 
 template <class E, bool WIDE>
 __global__ __launch_bounds__(kBlock) void matrix_kernel(MatrixParams p) {
+    constexpr bool SHORT = sizeof(E) == 2;
     __shared__ uint32_t tops[16][kGroup];
     __shared__ __attribute__((aligned(16))) uint8_t tile[kGroup * kTurnStride];
     const int64_t r0 = (int64_t)(blockIdx.x / p.col_tiles) * kGroup, c0 = (int64_t)(blockIdx.x % p.col_tiles) * kGroup;
@@ -207,17 +209,34 @@ __global__ __launch_bounds__(kBlock) void matrix_kernel(MatrixParams p) {
         for (int i = 0; i < 8; ++i) {
             const int64_t r = r0 + 8 * tr + i;
             const Scale s = p.square ? whole : scale_of(row_largest<16>(largest(v[i])), p.pow2);
-            straight[i] = codes_of(v[i], s);
-            if (p.out.codes && r < p.R) {
+            straight[i] = codes_of<SHORT>(v[i], s);
+            if (p.out.codes && r < p.R && tc == 0 && !p.square)
+                p.out.scale[r * p.out.scale_row_stride + c0 / kGroup * p.out.scale_block_stride] = s.scale;
+        }
+    }
+    if (p.out.codes) {
+        uint8_t* const to = p.out.codes + (r0 + 8 * tr) * p.out.row_stride + c0 + 8 * tc;
+        // Sixteen bytes a lane: neighbours exchange halves of two rows (even lanes keep the first).
+        if (p.wide_out && c0 + kGroup <= p.C) {
+            const bool odd = tc & 1;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const uint2 mine = odd ? straight[i + 1] : straight[i], give = odd ? straight[i] : straight[i + 1];
+                const uint2 got = {(uint32_t)gvr_dev::dpp_i<gvr_dev::kQuadSwap1>(0, (int)give.x),
+                                   (uint32_t)gvr_dev::dpp_i<gvr_dev::kQuadSwap1>(0, (int)give.y)};
+                if (r0 + 8 * tr + i + odd < p.R)
+                    *reinterpret_cast<uint4*>(to + (i + odd) * p.out.row_stride - 8 * odd) =
+                        odd ? uint4{got.x, got.y, mine.x, mine.y} : uint4{mine.x, mine.y, got.x, got.y};
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
                 const uint32_t w[2] = {straight[i].x, straight[i].y};
-                if (left > 0) put_bytes<8>(p.out.codes + r * p.out.row_stride + c0 + 8 * tc, w, left);
-                if (tc == 0 && !p.square)
-                    p.out.scale[r * p.out.scale_row_stride + c0 / kGroup * p.out.scale_block_stride] = s.scale;
+                if (r0 + 8 * tr + i < p.R && left > 0) put_bytes<8>(to + i * p.out.row_stride, w, left);
             }
         }
     }
     if (!p.turned.codes) return;
-    Scale col[8];
     if (!p.square) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -238,8 +257,6 @@ __global__ __launch_bounds__(kBlock) void matrix_kernel(MatrixParams p) {
                     scale_of(m, p.pow2).scale;
         }
         __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) col[j] = scale_of(tops[0][8 * tc + j], p.pow2);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -255,7 +272,7 @@ __global__ __launch_bounds__(kBlock) void matrix_kernel(MatrixParams p) {
             f8 y;
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = v[i][j];
-            c = codes_of(y, col[j]);
+            c = codes_of<SHORT>(y, scale_of(tops[0][8 * tc + j], p.pow2));
         }
         *reinterpret_cast<uint2*>(tile + (8 * tc + j) * kTurnStride + 8 * tr) = c;
     }
@@ -341,6 +358,7 @@ gvr_status gvr_fp8_quantize_matrix(const void* x, int64_t x_stride, int32_t dtyp
     p.turned = transposed ? *transposed : none;
     p.col_tiles = (uint32_t)gvr_fp8::groups_of(C);
     p.pow2 = flags & GVR_FP8_POW2, p.square = flags & GVR_FP8_SQUARE;
+    p.wide_out = ((uintptr_t)p.out.codes & 15) == 0 && p.out.row_stride % 16 == 0;
     const unsigned blocks = (unsigned)(gvr_fp8::groups_of(R) * gvr_fp8::groups_of(C));
     const int size = gvr_rot::dtype_size(dtype);
     const bool wide = ((uintptr_t)x & 15) == 0 && x_stride % (16 / size) == 0;
