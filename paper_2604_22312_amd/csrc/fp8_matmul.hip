@@ -649,10 +649,13 @@ gvr_status gvr_fp8_matmul_workspace(const gvr_fp8_matrix* a, const gvr_fp8_matri
     *bytes = 0;
     const gvr_status st = gvr_fp8::check_matmul(a, b, M, N, K, false);
     if (st != GVR_OK || M == 0 || N == 0) return st;
-    gvr_fp8::MatmulPlan plan;
-    const gvr_status fits = gvr_fp8::plan_matmul(*a, *b, M, N, K, false, (size_t)-1, &plan);
-    if (fits == GVR_OK) *bytes = plan.workspace;
-    return fits;
+    for (const bool wide : {false, true}) {   // (float32 results have no 256 x 256 tiles, and may be split otherwise)
+        gvr_fp8::MatmulPlan plan;
+        const gvr_status fits = gvr_fp8::plan_matmul(*a, *b, M, N, K, wide, (size_t)-1, &plan);
+        if (fits != GVR_OK) return fits;
+        if (plan.workspace > *bytes) *bytes = plan.workspace;
+    }
+    return GVR_OK;
 }
 
 gvr_status gvr_fp8_matmul(const gvr_fp8_matrix* a, const gvr_fp8_matrix* b, int64_t M, int64_t N, int64_t K, void* out,
