@@ -171,7 +171,7 @@ inline gvr_status plan_matmul(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, 
     if (tile_rows(a, 256, K) && tile_rows(b, 256, K)) {
         // Few rows of A: the kernels without tiles (the times are at them), with two tiles of B's rows to a workgroup
         // where that still gives one to each compute unit (1 x 8192 x 4096: 8.0 us, with one 8.6; 16 x: 9.7, 11.7).
-        if (M <= 16) {
+        if (M <= 16 && N <= 1 << 26) {   // (more rows of B: more threads than a launch has)
             p->shape = N >= 32 * kUnits ? kRowPairs : kRows;
         } else if (M <= 32 && N <= 16 * kUnits) {
             p->shape = kRows32;
@@ -180,8 +180,12 @@ inline gvr_status plan_matmul(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, 
             for (const Shape s : {kLow, kNarrow, kSquare, kLarge})
                 for (const int64_t n : {1, 2, 3, 4, 6, 8, 12, 16}) {
                     if (s == kLarge && wide) continue;   // (its sums are on the FP8 matrix cores)
-                    if (n > 1 && (steps < 4 * n || (double)n * M * N * 4 > (double)ws_bytes)) break;
-                    const double us = matmul_time(tiles_of(s), M, N, steps, n);
+                    const Tiles t = tiles_of(s);
+                    // (many workgroups need no splits: the kernel that joins them is launched over few rows)
+                    if (n > 1 && (steps < 4 * n || (double)n * M * N * 4 > (double)ws_bytes ||
+                                  ((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n) > 4 * kUnits))
+                        break;
+                    const double us = matmul_time(t, M, N, steps, n);
                     if (us < best) best = us, p->shape = s, splits = n;
                 }
         }
