@@ -1,11 +1,17 @@
 // fp8_matmul.hip -- products of 8-bit matrices with a scale per 128 elements,
 // behind include/gvr_fp8.h.
 //
-// A wave multiplies 16 rows of B with 64 rows of A, 128 elements at a time: one
-// gfx950 v_mfma_f32_16x16x128_f8f6f4 per 16 x 16 results gives the sum of a whole
-// block, which is scaled and added in float32. Lane l holds, of row l % 16 of
-// both operands, the 32 bytes from 32 (l / 16) on, and of the results column
-// l % 16 (a row of A) and rows 4 (l / 16) + i (of B).
+// One gfx950 v_mfma_f32_16x16x128_f8f6f4 multiplies 16 rows of B with 16 rows of A over
+// 128 elements and so gives the sums of a whole block, which are scaled and added in
+// float32: four multiply-adds of 4 cycles to a matrix instruction of 32. Lane l holds 32
+// bytes of row l % 16 of both operands, and of the results column l % 16 (a row of A)
+// and rows 4 (l / 16) + i (of B), so that a lane's results share A's scale and lie
+// together in memory.
+//
+// Three kinds of kernels, chosen by sizes and alignment in fp8_plan.h: few rows of A
+// (codes from memory to registers), tiles through LDS, and one for rows that are not
+// 16-byte aligned, which loads pieces of any alignment and shares nothing (128 x 4096 x
+// 4099 in packed rows: 115 us, in rows of 4112 bytes 16.7; one row of A 40.9 and 5.8).
 //
 // The FP8 matrix cores add the products of eight consecutive elements in fixed
 // point: measured, a product below 2^-13 of the largest of its eight is lost (with
@@ -143,6 +149,18 @@ __global__ __launch_bounds__(gvr_fp8::kThreads) void matmul_kernel(MatmulParams 
 // they write. drain<N>() waits until at most the newest N of them are under way,
 // and for every LDS read of the wave, ahead of the barrier after which buffers
 // change hands.
+//
+// 8192 x 8192 x 4096 into bfloat16 takes 243 to 251 us = 2.2 PFLOP/s (256 x 256 tiles; 183 us =
+// 3.0 PFLOP/s is a library product of the same codes with one scale for all). The card
+// runs at 1.9 GHz then, where the matrix instructions alone take 139 us. Measured in copies
+// that leave parts out: without fetching codes 20 us less, without the stores of the
+// results 22 us less (a compute unit stores its 128 KB in 5 us and multiplies
+// nothing meanwhile; its LDS holds one workgroup), the rest is waves waiting for each
+// other at the barrier. The steps that led here: additions in the shadow of the matrix
+// instructions (270 -> 260), the last tiles behind the barrier with loads spread out
+// (290 -> 275), results in 16-byte stores (252 -> 234).
+// Smaller products are bound by a compute unit's intake, some 30 to 60 GB/s, and by the
+// steps' latency: 128 x 8192 x 4096 17.5 us, of which joining two splits 4.
 typedef unsigned v2u __attribute__((ext_vector_type(2)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
@@ -228,11 +246,14 @@ __global__ __launch_bounds__((Tile<BM, BN, WM, WN, STAGES>::kThreads)) void tile
 
     // rows past the end read the last one and are not stored
     const int64_t left_m = min(p.M - m0, (int64_t)BM) - 1, left_n = min(p.N - n0, (int64_t)BN) - 1;
-    const v4u ra = uniform(resource(p.a.codes + m0 * p.a.row_stride, 0xFFFFFFFFu));
-    const v4u rb = uniform(resource(p.b.codes + n0 * p.b.row_stride, 0xFFFFFFFFu));
     const int64_t nb0 = n0 / p.b.rows_per_scale;
-    const v4u rsa = uniform(resource(p.a.scale + m0 * p.a.scale_row_stride, 0xFFFFFFFFu));
-    const v4u rsb = uniform(resource(p.b.scale + nb0 * p.b.scale_row_stride, 0xFFFFFFFFu));
+    v4u ra = uniform(resource(p.a.codes + m0 * p.a.row_stride, 0xFFFFFFFFu));
+    v4u rb = uniform(resource(p.b.codes + n0 * p.b.row_stride, 0xFFFFFFFFu));
+    v4u rsa = uniform(resource(p.a.scale + m0 * p.a.scale_row_stride, 0xFFFFFFFFu));
+    v4u rsb = uniform(resource(p.b.scale + nb0 * p.b.scale_row_stride, 0xFFFFFFFFu));
+    // (a scalar register that a vector instruction has written may be read by a load five states later; the compiler does not
+    // count them for loads in assembly)
+    asm volatile("s_nop 4" : "+s"(ra), "+s"(rb), "+s"(rsa), "+s"(rsb));
     const uint32_t base = uniform((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds);
     // A wave's loads are of eight consecutive rows each, first kLoadsA of A's, then of B's: the first ones' offsets, and the last rows'.
     const uint32_t chunk = 16 * ((lane & 7) ^ (lane >> 3)), a_stride = (uint32_t)p.a.row_stride, b_stride = (uint32_t)p.b.row_stride;

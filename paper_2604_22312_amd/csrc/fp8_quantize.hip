@@ -10,7 +10,12 @@
 // exchanges, a column's goes through LDS; the transposed codes are turned in LDS
 // and leave as 16 bytes of a column.
 //
-// Bound by HBM.
+// Bound by HBM where there is much (8192 x 4096 bfloat16 with eight elements a thread
+// at 24.2 us, sixteen 20.7 us = 4.9 TB/s, a copy's rate; both directions of 4099 x 4096
+// float32 26 us = 3.8 TB/s, of 4096 x 4096 bfloat16 23.8 us, 13 at a copy's rate: all
+// its workgroups run at once, each a chain of load, search, exchange and store), else by
+// the launch and its loads one after the other: slot, position, table row and element (one
+// key of 128 with its rotation 2.2 us on the device, 128 x 64 queries 3.8).
 
 #include <hip/hip_runtime.h>
 
