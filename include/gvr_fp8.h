@@ -115,10 +115,12 @@ gvr_status gvr_fp8_quantize_matrix(const void* x, int64_t x_stride, int32_t dtyp
  *
  * workspace: 16-byte aligned device memory of ws_bytes, used by this call only
  * while it runs (no clearing needed), for products whose sum is split over several
- * workgroups; gvr_fp8_matmul_workspace says how much (0: not split). Less than
- * that lowers the split, NULL with 0 bytes runs unsplit; the bits then differ by
- * the order of the float32 sums.
- * Any alignment and strides (16-byte aligned rows take the wide loads).
+ * workgroups, and for copies of codes whose rows are not 16-byte aligned;
+ * gvr_fp8_matmul_workspace says how much (0: neither). Less than that lowers the split
+ * and multiplies such codes where they are, which is slower, NULL with 0 bytes does
+ * both; the bits then differ by the order of the float32 sums.
+ * Any alignment and strides (16-byte aligned rows take the wide loads; the workspace
+ * depends on the alignment of the matrices that it is asked for).
  * Errors: GVR_ERR_INVALID_ARG (a NULL or misaligned required pointer, a negative
  * size, a bad dtype or rows_per_scale, a workspace NULL with bytes),
  * GVR_ERR_TOO_LONG (M, N or K above 2^31 - 16, or a grid of 2^32 threads or more),

@@ -195,7 +195,6 @@ inline gvr_status plan_matmul(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, 
     p->tiles_m = (M + t.m - 1) / t.m;
     p->tiles_n = (N + t.n - 1) / t.n;   // (each at most 2^27)
     if (p->shape == kRows && p->tiles_n < kUnits) p->threads = 1024;   // (more waves where workgroups are few)
-    // SWEEP
     p->steps_each = (steps + splits - 1) / splits;
     if (splits > 1) p->steps_each = (p->steps_each + 3) / 4 * 4;   // (scales come four at a time)
     p->splits = p->steps_each ? (steps + p->steps_each - 1) / p->steps_each : 1;
@@ -203,6 +202,55 @@ inline gvr_status plan_matmul(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, 
     p->workspace = p->splits > 1 ? (size_t)p->splits * M * N * 4 : 0;
     p->workgroups = p->tiles_m * p->tiles_n * p->splits;
     return p->workgroups * p->threads > 0xFFFFFFFFll ? GVR_ERR_TOO_LONG : GVR_OK;
+}
+
+// A product whose rows 16-byte loads cannot serve: its codes are copied to rows that
+// they can, in the workspace, if that has room, and the copies are multiplied. Packed
+// rows of both, copied and where they are: 1 x 64 x 101 6.1 us and 6.3, 1 x 4096 x 4099
+// 15.6 and 41, 128 x 4096 x 4099 25 and 115, 4096 x 4096 x 101 16.8 and 70, 4096 x 4096 x
+// 4099 83 and 1760.
+struct Product {
+    MatmulPlan plan;
+    bool copied[2];       // A, B
+    int64_t row_stride;   // of the copies
+    size_t at[2], parts;  // where the copies and the splits' parts begin
+    size_t workspace;     // bytes in all
+};
+
+inline bool wide_rows(const gvr_fp8_matrix& m, int64_t K) {
+    return ((uintptr_t)m.codes & 15) == 0 && m.row_stride % 16 == 0 && m.row_stride >= 0 && m.row_stride * 256 + K < kMaxCount;
+}
+
+inline gvr_status plan_product(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, int64_t M, int64_t N, int64_t K, bool wide,
+                               size_t ws_bytes, Product* p) {
+    const int64_t rows[2] = {M, N}, chunks = (K + 15) / 16;
+    gvr_fp8_matrix m[2] = {a, b};
+    p->row_stride = 16 * chunks;
+    p->parts = 0;
+    bool any = false, room = K > 0;
+    int64_t items = 0;
+    for (int i = 0; i < 2; ++i) {
+        if (rows[i] <= 1) m[i].row_stride = 0;   // (there is no next row)
+        p->copied[i] = !wide_rows(m[i], K);
+        p->at[i] = p->parts;
+        if (!p->copied[i]) continue;
+        any = true;
+        room = room && rows[i] < (kMaxCount - items) / chunks;   // (the copying kernel counts in 32 bits)
+        if (!room) break;
+        items += rows[i] * chunks;
+        p->parts += ((size_t)rows[i] * p->row_stride + 255) / 256 * 256;
+        m[i].codes = nullptr, m[i].row_stride = p->row_stride;
+    }
+    if (!any || (room && p->parts <= ws_bytes)) {
+        const gvr_status st = plan_matmul(m[0], m[1], M, N, K, wide, ws_bytes - p->parts, &p->plan);
+        p->workspace = p->parts + p->plan.workspace;
+        if (!any || (st == GVR_OK && p->plan.shape != kAnyShape)) return st;
+    }
+    p->copied[0] = p->copied[1] = false;
+    p->parts = 0;
+    const gvr_status st = plan_matmul(a, b, M, N, K, wide, ws_bytes, &p->plan);
+    p->workspace = p->plan.workspace;
+    return st;
 }
 
 }  // namespace gvr_fp8

@@ -204,7 +204,8 @@ def _matmul_workspace(sa, sb, M, N, K, dev):
 
 def gvr_fp8_matmul_workspace(a, a_scale, b, b_scale) -> int:
     """Bytes of workspace with which ``gvr_fp8_matmul`` of these matrices splits
-    its sums over the whole device (0: it does not split)."""
+    its sums over the whole device and brings rows that are not 16-byte aligned into
+    line (0: it does neither)."""
     sa, sb, M, N, K = _matmul_operands(a, a_scale, b, b_scale)
     return _matmul_workspace(sa, sb, M, N, K, a.device)
 
@@ -279,7 +280,7 @@ def _product_workspace(M, N, K, per, device):
 
 def _rows_of(x):
     """x [...][C] as a matrix whose rows are contiguous."""
-    m = x.reshape(-1, x.shape[-1])
+    m = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
     return m.contiguous() if m.shape[1] > 1 and m.stride(1) != 1 else m
 
 
@@ -375,9 +376,16 @@ def gvr_fp8_linear(x, weight, weight_t=None):
     transposed=True)`` made, with that of W^T as ``weight_t``, which the gradient of
     x needs. x and the gradient of y are quantised by 128 elements along the axis
     that each product sums over; the rounding counts as the identity, and there is no
-    second derivative. y and the gradients have the types of x and of the weight."""
+    second derivative. y and the gradients have the types of x and of the weight.
+    A training step may be captured into a graph, on one condition that all autograd
+    nodes share: no graph that was recorded eagerly from the same leaves is alive
+    (their accumulation belongs to the stream that it was recorded on)."""
     _need(isinstance(x, torch.Tensor) and x.dim() >= 1 and x.dtype in DTYPES and x.is_cuda,
           "x must be a bfloat16, float16 or float32 tensor [...][K] on a GPU (there is no CPU path)")
+    _need(x.shape[-1] >= 1, "a row of x needs at least one element")
+    if not torch.is_grad_enabled():   # (nothing is kept, and no codes of the transposed are made, for a backward pass that cannot be)
+        x = x.detach()
+        weight = weight.detach() if isinstance(weight, torch.Tensor) else weight
     if isinstance(weight, torch.Tensor):
         _need(weight.dim() == 2 and weight.dtype in DTYPES and weight.device == x.device and weight.shape[1] == x.shape[-1],
               "weight must be a bfloat16, float16 or float32 tensor [N][%d] on %s" % (x.shape[-1], x.device))

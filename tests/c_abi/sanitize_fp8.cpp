@@ -55,6 +55,33 @@ int main() {
     }
     for (int s = kAnyShape; s <= kLarge; ++s) CHECK(shapes[s] > 100);
     CHECK(split > 1000);
+    int copied[3] = {};
+    for (int i = 0; i < 300000; ++i) {   // products: copies and parts lie in the workspace, one behind the other
+        const int64_t M = pick(1, (int64_t)1 << pick(0, 31)), N = pick(1, (int64_t)1 << pick(0, 31)), K = pick(0, (int64_t)1 << pick(0, 31));
+        if (M > kMaxCount || N > kMaxCount || K > kMaxCount) continue;
+        const int64_t blocks = groups_of(K);
+        gvr_fp8_matrix a = {(uint8_t*)(uintptr_t)(pick(0, 1) ? 4096 : 4097), pick(0, 1) ? K : (K + 15) / 16 * 16, nullptr, blocks, 1, 1, 0};
+        gvr_fp8_matrix b = {(uint8_t*)(uintptr_t)4096, pick(0, 1) ? -K : (K + 15) / 16 * 16, nullptr, blocks, 1, 128, 0};
+        const size_t most = pick(0, 3) ? (size_t)-1 : (size_t)pick(0, (int64_t)1 << pick(0, 34));
+        Product p;
+        if (plan_product(a, b, M, N, K, pick(0, 1), most, &p) != GVR_OK) continue;
+        CHECK(p.workspace <= most && p.workspace == p.parts + p.plan.workspace && p.parts % 256 == 0);
+        size_t end = 0, items = 0;
+        for (int k = 0; k < 2; ++k)
+            if (p.copied[k]) {
+                const int64_t rows = k ? N : M;
+                CHECK(p.plan.shape != kAnyShape && p.row_stride >= K && p.row_stride % 16 == 0 && p.at[k] == end && K > 0);
+                end += ((size_t)rows * p.row_stride + 255) / 256 * 256;
+                items += (size_t)rows * (p.row_stride / 16);
+            }
+        CHECK(end == p.parts && items < ((size_t)1 << 31));
+        if (p.plan.shape != kAnyShape) {   // what is read by 16 bytes is aligned
+            CHECK(p.copied[0] || ((uintptr_t)a.codes % 16 == 0 && (M == 1 || a.row_stride % 16 == 0)));
+            CHECK(p.copied[1] || N == 1 || (b.row_stride % 16 == 0 && b.row_stride >= 0));
+        }
+        ++copied[p.copied[0] + p.copied[1]];
+    }
+    CHECK(copied[0] > 1000 && copied[1] > 1000 && copied[2] > 1000);
     for (int i = 0; i < 2000000; ++i) {
         const uint32_t d = (uint32_t)pick(1, (int64_t)1 << pick(0, 30)), n = (uint32_t)pick(0, 0x7FFFFFFF >> pick(0, 30));
         const Divisor v = divisor(d);

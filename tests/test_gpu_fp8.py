@@ -347,3 +347,45 @@ def test_a_sum_over_many_tokens_is_held_in_32_bits(G):
     out = G.gvr_fp8_matmul(a, s, a, s, dtype=torch.float32)
     assert (out == K).all()   # (whole numbers below 2^24: exact in any order)
     assert UNIT["f32"] < 1
+
+
+@pytest.mark.parametrize("M,N,K,per", [(1, 300, 1001, 128), (20, 1, 1001, 1), (70, 257, 401, 128), (300, 520, 1153, 1)])
+def test_rows_that_are_not_aligned(G, M, N, K, per):
+    """Packed and shifted rows of either matrix, copied in a workspace or multiplied where they are; a matrix of one row
+    has no row stride; what lies beside rows is not read into results (it is NaN)."""
+    note("fp8 unaligned %d %d %d" % (M, N, K))
+    rng = np.random.default_rng(M + K)
+    b, sb, cb, hb = matrix(rng, N, K, per, pad=-K % 16)
+    a, sa, ca, ha = matrix(rng, M, K, pad=-K % 16)
+
+    def shifted(c, by, stride):
+        store = torch.full((c.shape[0] * stride + by + 64,), 0x7F, dtype=torch.uint8, device=DEV)
+        v = store[by:].as_strided(c.shape, (stride, 1))
+        return v.copy_(c)
+    for dtype in ("bf16", "f32"):
+        ref, mag = O.product(ca, ha, cb, hb, per)
+        bound = product_bound(mag, ref, K, dtype, cut_off(O.values(ca, ha), O.values(cb, hb, per)))
+        aligned = G.gvr_fp8_matmul(a, sa, b, sb, dtype=TORCH[dtype])
+        close(aligned, ref, bound)
+        for a2, b2 in ((shifted(a, 0, K), b), (a, shifted(b, 0, K)), (shifted(a, 3, K + 1), shifted(b, 1, K + 22)),
+                       (shifted(a, 8, K + 7), shifted(b, 16, K))):
+            n = G.gvr_fp8_matmul_workspace(a2, sa, b2, sb)
+            for size in (0, n // 2, n):   # (the last as much as it asks for)
+                ws = torch.full((size,), 0x7F, dtype=torch.uint8, device=DEV)
+                out = G.gvr_fp8_matmul(a2, sa, b2, sb, dtype=TORCH[dtype], workspace=ws)
+                close(out, ref, bound)
+            assert torch.equal(out, G.gvr_fp8_matmul(a2, sa, b2, sb, dtype=TORCH[dtype]))
+
+
+def test_linear_keeps_nothing_without_gradients(G):
+    note("fp8 linear no grad")
+    torch.manual_seed(2)
+    x = torch.randn((130, 300), device=DEV, requires_grad=True)
+    w = torch.randn((70, 300), device=DEV, requires_grad=True)
+    y = G.gvr_fp8_linear(x, w)
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            z = G.gvr_fp8_linear(x, w)
+        assert not z.requires_grad and torch.equal(z, y.detach())
+    with pytest.raises(ValueError):
+        G.gvr_fp8_linear(x[:, :0], w[:, :0])
