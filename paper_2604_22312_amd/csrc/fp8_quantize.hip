@@ -336,7 +336,8 @@ gvr_status gvr_fp8_quantize(const gvr_heads* x, int32_t dtype, int64_t T, int32_
             mode = p.rot % 16 == 0 ? kHalf : kAny;
     }
     const int64_t blocks = (int64_t)H * gvr_fp8::groups_of(D);
-    // Sixteen elements a thread where that leaves threads enough to fill the device.
+    // Sixteen elements a thread where that leaves threads enough to fill the device (8192 x 4096 bfloat16, not in the caches:
+    // 20.7 us, with eight 24.2; from 256 to 2048 rows of 4096 the two differ by 0.5 us at most, either way).
     if (mode == kNoTurn && ((uintptr_t)p.codes & 15) == 0 && p.ct % 16 == 0 && p.ch % 16 == 0 &&
         T * blocks >= (int64_t)256 * 2048 / 8)
         mode = kNoTurn16;

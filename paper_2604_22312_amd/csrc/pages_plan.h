@@ -45,7 +45,8 @@ inline gvr_status check(const gvr_page_pool* p, const gvr_page_step_args* a, con
 
 // One workgroup does the whole step where it has at most this many requests and
 // rows, else it adds up the requests and two more kernels move the pages and fill
-// the rows.
+// the rows (one workgroup and three kernels: 64 requests and 128 rows 4.4 us and 9.5, 1024
+// and 2048 9.1 and 11.5, 300 and 4096 10.5 both, 300 and 16384 22.6 and 10.5).
 constexpr int kSmallRequests = 1024, kSmallRows = 2048;
 inline bool small_step(int requests, int64_t T) { return requests <= kSmallRequests && T <= kSmallRows; }
 
