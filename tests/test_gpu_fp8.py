@@ -389,3 +389,32 @@ def test_linear_keeps_nothing_without_gradients(G):
         assert not z.requires_grad and torch.equal(z, y.detach())
     with pytest.raises(ValueError):
         G.gvr_fp8_linear(x[:, :0], w[:, :0])
+
+
+@pytest.mark.parametrize("K", [100, 128, 200, 256, 300, 384, 500, 640, 1153])
+def test_many_large_tiles(G, K):
+    """More tiles of 256 x 256 than compute units, with every number of steps at a tile's begin and end; a NaN row and a NaN
+    column stay in theirs; results in aligned and in other rows are the same."""
+    note("fp8 many tiles %d" % K)
+    M, N = 8100, 8192
+    rng = np.random.default_rng(K)
+    a, sa, ca, ha = matrix(rng, M, K, pad=-K % 16)
+    b, sb, cb, hb = matrix(rng, N, K, 128, pad=-K % 16)
+    a[4000, K - 1] = 0x7F
+    b[7000, 0] = 0xFF
+    dtype = ["bf16", "f16"][K % 8 // 4]
+    out = G.gvr_fp8_matmul(a, sa, b, sb, dtype=TORCH[dtype])
+    nan = torch.isnan(out)
+    assert nan[4000].all() and nan[:, 7000].all() and int(nan.sum()) == M + N - 1
+    rows = np.unique(np.concatenate([rng.integers(0, M, 100), [0, 255, 256, 8063, 8064, 8099]]))
+    rows = rows[rows != 4000]
+    keep = np.delete(np.arange(N), 7000)
+    ref, mag = O.product(ca[rows], ha[rows], cb, hb, 128)
+    cut = cut_off(O.values(ca[rows], ha[rows]), O.values(cb, hb, 128))
+    got = out[torch.from_numpy(rows).to(DEV)][:, torch.from_numpy(keep).to(DEV)]
+    close(got, ref[:, keep], product_bound(mag, ref, K, dtype, cut)[:, keep])
+    store = torch.full((M, N + 3), 7.0, dtype=TORCH[dtype], device=DEV)
+    G.gvr_fp8_matmul(a, sa, b, sb, out=store[:, 1:N + 1])
+    assert torch.equal(store[:, 1:N + 1].nan_to_num(3.0), out.nan_to_num(3.0))
+    assert (store[:, 0] == 7).all() and (store[:, N + 1:] == 7).all()
+    assert torch.equal(G.gvr_fp8_matmul(a, sa, b, sb, dtype=TORCH[dtype]).nan_to_num(3.0), out.nan_to_num(3.0))
