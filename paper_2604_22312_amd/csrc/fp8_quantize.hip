@@ -10,12 +10,12 @@
 // exchanges, a column's goes through LDS; the transposed codes are turned in LDS
 // and leave as 16 bytes of a column.
 //
-// Bound by HBM where there is much (8192 x 4096 bfloat16 with eight elements a thread
-// at 24.2 us, sixteen 20.7 us = 4.9 TB/s, a copy's rate; both directions of 4099 x 4096
-// float32 26 us = 3.8 TB/s, of 4096 x 4096 bfloat16 23.8 us, 13 at a copy's rate: all
-// its workgroups run at once, each a chain of load, search, exchange and store), else by
-// the launch and its loads one after the other: slot, position, table row and element (one
-// key of 128 with its rotation 2.2 us on the device, 128 x 64 queries 3.8).
+// Bound by HBM where there is much (8192 x 4096 bfloat16 18.7 us, a copy's rate and a
+// little more), the other direction beside it by a chain of load, search, exchange and
+// store in each workgroup, all of which run at once (4099 x 4096 float32 26 us, 20 at a copy's
+// rate; 4096 x 4096 bfloat16 22, 13 at a copy's rate); else by the launch and the loads
+// one after the other: slot, position, table row and element (one key of 128 with its
+// rotation 2.2 us on the device, 128 x 64 queries 4.1).
 
 #include <hip/hip_runtime.h>
 
@@ -51,8 +51,11 @@ struct HeadsParams {
 
 enum { kNoTurn, kHalf, kInter, kAny, kNoTurn16 };   // rotations; kAny also serves rows of any alignment and length
 
+// Where HBM is the bound, six waves to a SIMD, not eight, and codes that go past the caches (4096 x 4096 bfloat16 14.3 -> 12.9
+// us, 8192 x 4096 23.7 -> 22.1, 16384 x 4096 40.5 -> 39.3).
 template <class E, int MODE, int PER>
-__global__ __launch_bounds__(kBlock) void heads_kernel(HeadsParams p) {
+__global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(PER == 16 ? 6 : 1, PER == 16 ? 6 : 8)))
+void heads_kernel(HeadsParams p) {
     constexpr bool WIDE = MODE != kAny;
     constexpr int LANES = kGroup / PER;   // of a block
     const uint32_t idx = blockIdx.x * (uint32_t)kBlock + threadIdx.x;
@@ -121,7 +124,8 @@ __global__ __launch_bounds__(kBlock) void heads_kernel(HeadsParams p) {
     uint8_t* const out = p.codes + row * p.ct + h * p.ch + e;
     if constexpr (PER == 16) {
         const uint2 more = codes_of<SHORT>(w, sc);
-        if (left >= 16) *reinterpret_cast<uint4*>(out) = uint4{codes.x, codes.y, more.x, more.y};
+        typedef unsigned u4 __attribute__((ext_vector_type(4)));
+        if (left >= 16) __builtin_nontemporal_store(u4{codes.x, codes.y, more.x, more.y}, reinterpret_cast<u4*>(out));
         else if (left > 0) *reinterpret_cast<uint2*>(out) = codes;
     } else if constexpr (WIDE) {
         if (left > 0) *reinterpret_cast<uint2*>(out) = codes;
@@ -337,7 +341,7 @@ gvr_status gvr_fp8_quantize(const gvr_heads* x, int32_t dtype, int64_t T, int32_
     }
     const int64_t blocks = (int64_t)H * gvr_fp8::groups_of(D);
     // Sixteen elements a thread where that leaves threads enough to fill the device (8192 x 4096 bfloat16, not in the caches:
-    // 20.7 us, with eight 24.2; from 256 to 2048 rows of 4096 the two differ by 0.5 us at most, either way).
+    // 20.7 us when eight took 24.2; from 256 to 2048 rows of 4096 the two differ by 0.5 us at most, either way).
     if (mode == kNoTurn && ((uintptr_t)p.codes & 15) == 0 && p.ct % 16 == 0 && p.ch % 16 == 0 &&
         T * blocks >= (int64_t)256 * 2048 / 8)
         mode = kNoTurn16;
