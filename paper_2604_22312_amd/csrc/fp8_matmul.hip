@@ -546,7 +546,7 @@ __global__ __launch_bounds__(64 * WAVES) void rows_kernel(MatmulParams p) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) sb[4 * i + r] = p.b.scale + min(n0 + 16 * i + 4 * quarter + r, p.N - 1) * p.b.scale_row_stride;
     }
-    if constexpr (!BYROW) sb[0] = p.b.scale + n0 / kGroup * p.b.scale_row_stride;   // (16 NT rows from a multiple of 16 NT share it)
+    if constexpr (!BYROW) sb[0] = p.b.scale + min(n0, p.N - 1) / kGroup * p.b.scale_row_stride;   // (16 NT rows from a multiple of 16 NT share it)
     v4f acc[NT][MT] = {};
     auto add = [&](const v8i (&bv)[NT], const float (&fb)[BYROW ? 4 * NT : 1], const v8i (&av)[MT], const float (&fa)[MT]) {
 #pragma unroll

@@ -163,18 +163,41 @@ inline double matmul_time(const Tiles& t, int64_t M, int64_t N, int64_t steps, i
     return us;
 }
 
+// What a shape and a split come to as a launch. The kernels of few rows hold all of A's
+// and take a workgroup's rows of B from its number alone, so more tiles along A or a
+// split sum would run them past the end of B: a shape that cannot do these sizes is an
+// error, and nothing is launched.
+inline gvr_status lay_out(Shape shape, int64_t splits, int64_t M, int64_t N, int64_t K, bool wide, MatmulPlan* p) {
+    const int64_t steps = groups_of(K);
+    const Tiles t = tiles_of(shape);
+    p->shape = shape;
+    p->threads = t.threads;
+    p->tiles_m = (M + t.m - 1) / t.m;
+    p->tiles_n = (N + t.n - 1) / t.n;   // (each at most 2^27)
+    if (shape == kRows && p->tiles_n < kUnits) p->threads = 1024;   // (more waves where workgroups are few)
+    p->steps_each = (steps + splits - 1) / splits;
+    if (splits > 1) p->steps_each = (p->steps_each + 3) / 4 * 4;   // (scales come four at a time)
+    p->splits = p->steps_each ? (steps + p->steps_each - 1) / p->steps_each : 1;
+    p->band = 4;   // (8192 x 8192 x 4096: 243 us, of 2 and 8 246 and 245, of 16 248; 16384 x 8192 x 4096: 467, 485 and 479, 493)
+    p->workspace = p->splits > 1 ? (size_t)p->splits * M * N * 4 : 0;
+    p->workgroups = p->tiles_m * p->tiles_n * p->splits;
+    const bool rows = shape == kRows || shape == kRowPairs || shape == kRows32;
+    if ((rows && p->tiles_m != 1) || (shape < kLow && p->splits != 1) || (shape == kLarge && wide)) return GVR_ERR_INVALID_ARG;
+    return p->workgroups * p->threads > 0xFFFFFFFFll ? GVR_ERR_TOO_LONG : GVR_OK;
+}
+
 inline gvr_status plan_matmul(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, int64_t M, int64_t N, int64_t K, bool wide,
                               size_t ws_bytes, MatmulPlan* p) {
     const int64_t steps = groups_of(K);
     int64_t splits = 1;
-    p->shape = kAnyShape;
+    Shape shape = kAnyShape;
     if (tile_rows(a, 256, K) && tile_rows(b, 256, K)) {
         // Few rows of A: the kernels without tiles (the times are at them), with two tiles of B's rows to a workgroup
         // where that still gives one to each compute unit (1 x 8192 x 4096: 8.0 us, with one 8.6; 16 x: 9.7, 11.7).
         if (M <= 16 && N <= 1 << 26) {   // (more rows of B: more threads than a launch has)
-            p->shape = N >= 32 * kUnits ? kRowPairs : kRows;
+            shape = N >= 32 * kUnits ? kRowPairs : kRows;
         } else if (M <= 32 && N <= 16 * kUnits) {
-            p->shape = kRows32;
+            shape = kRows32;
         } else {
             double best = 1e300;
             for (const Shape s : {kLow, kNarrow, kSquare, kLarge})
@@ -186,22 +209,11 @@ inline gvr_status plan_matmul(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, 
                                   ((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n) > 4 * kUnits))
                         break;
                     const double us = matmul_time(t, M, N, steps, n);
-                    if (us < best) best = us, p->shape = s, splits = n;
+                    if (us < best) best = us, shape = s, splits = n;
                 }
         }
     }
-    const Tiles t = tiles_of(p->shape);
-    p->threads = t.threads;
-    p->tiles_m = (M + t.m - 1) / t.m;
-    p->tiles_n = (N + t.n - 1) / t.n;   // (each at most 2^27)
-    if (p->shape == kRows && p->tiles_n < kUnits) p->threads = 1024;   // (more waves where workgroups are few)
-    p->steps_each = (steps + splits - 1) / splits;
-    if (splits > 1) p->steps_each = (p->steps_each + 3) / 4 * 4;   // (scales come four at a time)
-    p->splits = p->steps_each ? (steps + p->steps_each - 1) / p->steps_each : 1;
-    p->band = 4;   // (8192 x 8192 x 4096: 243 us, of 2 and 8 246 and 245, of 16 248; 16384 x 8192 x 4096: 467, 485 and 479, 493)
-    p->workspace = p->splits > 1 ? (size_t)p->splits * M * N * 4 : 0;
-    p->workgroups = p->tiles_m * p->tiles_n * p->splits;
-    return p->workgroups * p->threads > 0xFFFFFFFFll ? GVR_ERR_TOO_LONG : GVR_OK;
+    return lay_out(shape, splits, M, N, K, wide, p);
 }
 
 // A product whose rows 16-byte loads cannot serve: its codes are copied to rows that
