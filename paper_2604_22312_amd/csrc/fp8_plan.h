@@ -7,6 +7,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "gvr_fp8.h"
 #include "rotary_plan.h"
 
