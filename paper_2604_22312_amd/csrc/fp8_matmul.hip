@@ -172,14 +172,19 @@ DEV v4u resource(const void* base, uint32_t bytes) {
 DEV uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 DEV v4u uniform(v4u v) { return v4u{uniform(v[0]), uniform(v[1]), uniform(v[2]), uniform(v[3])}; }
 
+// (both say that they write m0: the compiler keeps numbers of its own there for other instructions. That it warns of naming
+// a register that it hands out by itself is about asm that expects to find its own number there afterwards)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 DEV void fetch16(uint32_t lds, v4u rsrc, uint32_t voffset, uint32_t soffset) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 :: "s"(lds), "v"(voffset), "s"(rsrc), "s"(soffset) : "memory");
+                 :: "s"(lds), "v"(voffset), "s"(rsrc), "s"(soffset) : "m0", "memory");
 }
 DEV void fetch4(uint32_t lds, v4u rsrc, uint32_t voffset, uint32_t soffset) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
-                 :: "s"(lds), "v"(voffset), "s"(rsrc), "s"(soffset) : "memory");
+                 :: "s"(lds), "v"(voffset), "s"(rsrc), "s"(soffset) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 template <int N>
 DEV void drain() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
