@@ -33,7 +33,8 @@
  *   taken [R] int32         n_r, 0 for a request that was not served
  *   positions [T] int32     p
  *   slots [T] int64         block_table[r][p / P] * P + p % P
- *   dense [T] int64         r * ld + p (the row of a cache [R][ld][...])
+ *   dense [T] int64         r * ld + p (the row of a cache [R][ld][...]), -1 where
+ *                           p >= ld: the request has no such row there
  *   row_len [T] int32       p + 1: the tokens that the row sees
  * All other rows up to T (padding, requests that were not served): position 0,
  * slot -1, dense -1, row_len 0, which the append skips and the Top-K and the

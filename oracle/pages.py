@@ -47,7 +47,8 @@ class Pool:
             taken.append(n if served else 0)
             for i in range(taken[-1]):
                 p = k + i
-                rows[start + i] = (p, self.tables[r][p // self.P] * self.P + p % self.P, r * ld + p, p + 1)
+                rows[start + i] = (p, self.tables[r][p // self.P] * self.P + p % self.P, r * ld + p if p < ld else -1,
+                                   p + 1)
             start += n
         self.free += reversed(given)
         starts.append(min(start, T))

@@ -196,7 +196,7 @@ DEV void fill_row(const StepParams& p, const Hand& h, const int32_t* starts, int
     if (keep >= 0) {
         pos = keep + (int32_t)(t - h.start[r]);
         see = pos + 1;
-        dense = r * p.a.ld + pos;
+        dense = pos < p.a.ld ? r * p.a.ld + pos : -1;   // (behind them the next request's rows begin)
         if (p.a.slots) {
             const int64_t page = p.pool.block_table[r * p.pool.width + (pos >> p.lg_page)];
             if (page >= 0 && page < (int64_t)1 << (31 - p.lg_page))

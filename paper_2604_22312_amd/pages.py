@@ -122,7 +122,7 @@ def gvr_page_step(pool, new_len, tokens, keep=None, ld=None, workspace=None, str
     ``taken`` (new_len, or 0 for a request that was not served: no pages, no
     place in its table or no rows left), and for every row ``positions``,
     ``slots`` for the append, ``dense`` = r * ld + position for a cache
-    [requests][ld] (None without ``ld``) and ``row_len`` = position + 1 for the
+    [requests][ld] (-1 where the position is ld or more; None without ``ld``) and ``row_len`` = position + 1 for the
     indexer. Rows of nobody: 0, -1, -1 and 0. ``workspace``: device memory of
     ``gvr_page_step_workspace`` bytes, allocated for the call if None."""
     return prepare_gvr_page_step(pool, new_len, tokens, keep, ld, workspace, stream)()
