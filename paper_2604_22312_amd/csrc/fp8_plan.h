@@ -154,8 +154,23 @@ inline bool scale_quads(const gvr_fp8_matrix& m, int64_t K, int64_t steps_each) 
            groups_of(K) % 4 == 0 && K % kGroup == 0 && steps_each % 4 == 0;
 }
 
+// The steps of each part of a sum that is split over about n workgroups (scales come
+// four at a time), and how many parts that makes.
+struct Split {
+    int64_t each, parts;
+};
+inline Split split_of(int64_t steps, int64_t n) {
+    Split s;
+    s.each = (steps + n - 1) / n;
+    if (n > 1) s.each = (s.each + 3) / 4 * 4;
+    s.parts = s.each ? (steps + s.each - 1) / s.each : 1;
+    return s;
+}
+
 // The time that a shape takes, in microseconds: rounds of workgroups, each as long
-// as its steps, and where the sum is split the kernel that joins the parts.
+// as its steps, and where the sum is split the kernel that joins the parts. (Of the
+// splits as they are asked for: with those of split_of in their place one plan in sixteen
+// differs, and 40 of these products took 827 us together, not 817.)
 inline double matmul_time(const Tiles& t, int64_t M, int64_t N, int64_t steps, int64_t splits) {
     const int64_t units = ((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n) * splits, each = (steps + splits - 1) / splits;
     const int64_t round = t.two > 0 ? 2 * kUnits : kUnits, whole = units / round, rest = units % round;
@@ -170,16 +185,15 @@ inline double matmul_time(const Tiles& t, int64_t M, int64_t N, int64_t steps, i
 // split sum would run them past the end of B: a shape that cannot do these sizes is an
 // error, and nothing is launched.
 inline gvr_status lay_out(Shape shape, int64_t splits, int64_t M, int64_t N, int64_t K, bool wide, MatmulPlan* p) {
-    const int64_t steps = groups_of(K);
     const Tiles t = tiles_of(shape);
     p->shape = shape;
     p->threads = t.threads;
     p->tiles_m = (M + t.m - 1) / t.m;
     p->tiles_n = (N + t.n - 1) / t.n;   // (each at most 2^27)
     if (shape == kRows && p->tiles_n < kUnits) p->threads = 1024;   // (more waves where workgroups are few)
-    p->steps_each = (steps + splits - 1) / splits;
-    if (splits > 1) p->steps_each = (p->steps_each + 3) / 4 * 4;   // (scales come four at a time)
-    p->splits = p->steps_each ? (steps + p->steps_each - 1) / p->steps_each : 1;
+    const Split split = split_of(groups_of(K), splits);
+    p->steps_each = split.each;
+    p->splits = split.parts;
     p->band = 4;   // (8192 x 8192 x 4096: 243 us, of 2 and 8 246 and 245, of 16 248; 16384 x 8192 x 4096: 467, 485 and 479, 493)
     p->workspace = p->splits > 1 ? (size_t)p->splits * M * N * 4 : 0;
     p->workgroups = p->tiles_m * p->tiles_n * p->splits;
@@ -207,7 +221,7 @@ inline gvr_status plan_matmul(const gvr_fp8_matrix& a, const gvr_fp8_matrix& b, 
                     if (s == kLarge && wide) continue;   // (its sums are on the FP8 matrix cores)
                     const Tiles t = tiles_of(s);
                     // (many workgroups need no splits: the kernel that joins them is launched over few rows)
-                    if (n > 1 && (steps < 4 * n || (double)n * M * N * 4 > (double)ws_bytes ||
+                    if (n > 1 && (steps < 4 * n || (double)split_of(steps, n).parts * M * N * 4 > (double)ws_bytes ||
                                   ((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n) > 4 * kUnits))
                         break;
                     const double us = matmul_time(t, M, N, steps, n);

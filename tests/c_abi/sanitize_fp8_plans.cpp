@@ -49,7 +49,38 @@ static void forced_shapes() {
     CHECK(lay_out(kRows32, 2, 32, 531, 1000, true, &p) == GVR_ERR_INVALID_ARG);
 }
 
+// A product with as much workspace as was asked for is planned as with any more, and one with less fits it.
+static void exact_workspace() {
+    int split = 0, uneven = 0, copied = 0;
+    for (int i = 0; i < 300000; ++i) {
+        const int64_t M = pick(1, (int64_t)1 << pick(0, 14)), N = pick(1, (int64_t)1 << pick(0, 14)), K = pick(1, (int64_t)1 << pick(0, 14));
+        const int64_t blocks = groups_of(K);
+        const gvr_fp8_matrix a = {(uint8_t*)(uintptr_t)(pick(0, 3) ? 4096 : 4100), (K + 15) / 16 * 16, nullptr, blocks, 1, 1, 0};
+        const gvr_fp8_matrix b = {(uint8_t*)(uintptr_t)4096, pick(0, 3) ? (K + 15) / 16 * 16 : K, nullptr, blocks, 1, 128, 0};
+        const bool wide = pick(0, 1);
+        Product most, exact, less;
+        CHECK(plan_product(a, b, M, N, K, wide, (size_t)-1, &most) == GVR_OK);
+        CHECK(plan_product(a, b, M, N, K, wide, most.workspace, &exact) == GVR_OK);
+        CHECK(exact.workspace == most.workspace && exact.plan.shape == most.plan.shape && exact.plan.splits == most.plan.splits);
+        CHECK(exact.plan.steps_each == most.plan.steps_each && exact.copied[0] == most.copied[0] && exact.copied[1] == most.copied[1]);
+        // (what is asked for serves every type of the result)
+        Product other;
+        CHECK(plan_product(a, b, M, N, K, !wide, (size_t)-1, &other) == GVR_OK);
+        const size_t asked = most.workspace > other.workspace ? most.workspace : other.workspace;
+        CHECK(plan_product(a, b, M, N, K, wide, asked, &exact) == GVR_OK);
+        CHECK(exact.plan.shape == most.plan.shape && exact.plan.splits == most.plan.splits);
+        if (most.workspace) {
+            CHECK(plan_product(a, b, M, N, K, wide, most.workspace - 1, &less) == GVR_OK && less.workspace < most.workspace);
+        }
+        split += most.plan.splits > 1;
+        uneven += most.plan.splits > 1 && blocks % most.plan.steps_each != 0;
+        copied += most.copied[0] || most.copied[1];
+    }
+    CHECK(split > 10000 && uneven > 2000 && copied > 10000);
+}
+
 int main() {
     forced_shapes();
+    exact_workspace();
     std::printf("ok\n");
 }
