@@ -270,11 +270,19 @@ def _check(name, status):
         raise GvrError(name, status)
 
 
+def _layout(m):
+    """Of an ``_Fp8Matrix``, what its product's workspace depends on beside its sizes."""
+    return (m.codes or 0) % 16, m.row_stride, m.scale_row_stride, m.scale_block_stride
+
+
 @functools.lru_cache(maxsize=4096)
-def _product_workspace(M, N, K, per, device):
-    """Bytes for split sums of a product of matrices as a ``_Block`` has them (their sizes alone decide)."""
+def _product_workspace(M, N, K, per, device, layout=None):
+    """Bytes of workspace of a product of matrices as a ``_Block`` has them (their sizes alone decide), or with a second one
+    of the caller's, of this ``_layout``."""
     b = _Block()
     sa, sb = b.matrix(M, K, 1), b.matrix(N, K, per)
+    if layout is not None:
+        sb = _Fp8Matrix(layout[0], layout[1], 0, layout[2], layout[3], per, 0)
     return _matmul_workspace(sa, sb, M, N, K, torch.device("cuda", device))
 
 
@@ -302,7 +310,7 @@ class _Linear(torch.autograd.Function):
             wq, wt = now.matrix(N, K, BLOCK), kept.matrix(K, N, BLOCK) if need_x else None
         else:
             wq, wt = _matrix_struct((codes, scale), "weight", N, K, BLOCK, dev), None
-        ws = _product_workspace(M, N, K, BLOCK, dev.index)
+        ws = _product_workspace(M, N, K, BLOCK, dev.index, _layout(wq) if weight is None else None)
         block, ws_at = now.place(dev, ws)
         saved = kept.place(dev)[0] if kept.size else None
         with _on_device(dev):
@@ -348,7 +356,7 @@ class _Linear(torch.autograd.Function):
         dq, dt = now.matrix(M, N, 1) if need_x else None, now.matrix(N, M, 1) if need_w else None
         dx = torch.empty((M, K), dtype=ctx.types[0], device=dev) if need_x else None
         dw = torch.empty((N, K), dtype=ctx.types[1], device=dev) if need_w else None
-        ws_x = _product_workspace(M, K, N, BLOCK, dev.index) if need_x else 0
+        ws_x = _product_workspace(M, K, N, BLOCK, dev.index, _layout(wt) if codes_t is not None else None) if need_x else 0
         ws_w = _product_workspace(N, K, M, 1, dev.index) if need_w else 0
         ws = max(ws_x, ws_w)   # (one after the other)
         block, ws_at = now.place(dev, ws)
