@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 from typing import NamedTuple
 
 import torch
@@ -288,7 +289,7 @@ def _product_workspace(M, N, K, per, device, layout=None):
 
 def _rows_of(x):
     """x [...][C] as a matrix whose rows are contiguous."""
-    m = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
+    m = x if x.dim() == 2 else x.reshape(math.prod(x.shape[:-1]), x.shape[-1])   # (C may be 0)
     return m.contiguous() if m.shape[1] > 1 and m.stride(1) != 1 else m
 
 
