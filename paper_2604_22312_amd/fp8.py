@@ -313,7 +313,7 @@ class _Linear(torch.autograd.Function):
             wq, wt = _matrix_struct((codes, scale), "weight", N, K, BLOCK, dev), None
         ws = _product_workspace(M, N, K, BLOCK, dev.index, _layout(wq) if weight is None else None)
         block, ws_at = now.place(dev, ws)
-        saved = kept.place(dev)[0] if kept.size else None
+        saved = kept.place(dev)[0] if kept.made else None
         with _on_device(dev):
             stream = _stream(None, dev)
             if need_w:

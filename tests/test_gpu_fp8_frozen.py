@@ -54,3 +54,17 @@ def test_layers_of_different_layouts_in_turn(G):  # noqa: F811
         for i in range(3):
             for w in ways:
                 assert torch.equal(G.gvr_fp8_linear(x, w), want)
+
+
+@pytest.mark.parametrize("shape", [(3, 60, 200), (7, 200), (200,), (0, 5, 200)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_layer_without_outputs(G, shape, dtype):  # noqa: F811
+    note("fp8 layer without outputs %s" % (shape,))
+    x = torch.randn(shape, device=DEV, dtype=dtype, requires_grad=True)
+    w = torch.randn((0, 200), device=DEV, requires_grad=True)
+    for f in (lambda: G.gvr_fp8_linear(x, w), lambda: G.gvr_fp8_linear(x, *G.gvr_fp8_quantize_matrix(w.detach(), square=True,
+                                                                                                   transposed=True))):
+        y = f()
+        assert y.shape == shape[:-1] + (0,) and y.dtype == dtype
+        got = torch.autograd.grad(y, (x, w), torch.ones_like(y), allow_unused=True)
+        assert got[0].shape == shape and (got[0] == 0).all() and (got[1] is None or got[1].shape == (0, 200))
