@@ -669,16 +669,14 @@ template <class E, bool BYROW>
 void launch_shape(const TileParams& t, const gvr_fp8::MatmulPlan& plan, hipStream_t s) {
     const dim3 grid((unsigned)plan.workgroups), block(plan.threads);
     auto go = [&](auto kernel, auto params) { hipLaunchKernelGGL(kernel, grid, block, 0, s, params); };
-    // Tiles into float32 read a scale for each row of B also where 128 rows share one: there is no kernel of their own.
-    constexpr bool EACH = BYROW || sizeof(E) == 4;
     switch (plan.shape) {
         case gvr_fp8::kAnyShape: go(matmul_kernel<E>, t.p); break;
         case gvr_fp8::kRows: plan.threads == 512 ? go(rows_kernel<E, BYROW, 1, 1, 4, 8>, t.p) : go(rows_kernel<E, BYROW, 1, 1, 4, 16>, t.p); break;
         case gvr_fp8::kRowPairs: go(rows_kernel<E, BYROW, 1, 2, 4, 8>, t.p); break;
         case gvr_fp8::kRows32: go(rows_kernel<E, BYROW, 2, 1, 4, 8>, t.p); break;
-        case gvr_fp8::kLow: go(tile_kernel<E, EACH, 64, 128, 64, 32, 3>, t); break;
-        case gvr_fp8::kNarrow: go(tile_kernel<E, EACH, 128, 64, 64, 32, 3>, t); break;
-        case gvr_fp8::kSquare: go(tile_kernel<E, EACH, 128, 128, 64, 64, 2>, t); break;
+        case gvr_fp8::kLow: go(tile_kernel<E, BYROW, 64, 128, 64, 32, 3>, t); break;
+        case gvr_fp8::kNarrow: go(tile_kernel<E, BYROW, 128, 64, 64, 32, 3>, t); break;
+        case gvr_fp8::kSquare: go(tile_kernel<E, BYROW, 128, 128, 64, 64, 2>, t); break;
         case gvr_fp8::kLarge:
             if constexpr (sizeof(E) == 2) go(tile_kernel<E, BYROW, 256, 256, 128, 64, 2>, t);
             break;
