@@ -16,6 +16,7 @@ from .binding import GvrError, _new, _on_device, _ptr, _stream
 from .kv4 import DTYPES, _cs, _Heads, _heads_tensor, _index, _need, _no_overlap, _RopeCs
 
 BLOCK = 128
+MAX_HEAD = 1 << 20   # elements of a head at most
 FP8_POW2, FP8_SQUARE = 1, 2
 
 _ready = False
@@ -67,7 +68,7 @@ def prepare_gvr_fp8_quantize(x, table=None, positions=None, interleaved=False, p
     xs = _heads_tensor(x3, "x")
     T, H, D = x3.shape
     dev = x.device
-    _need(1 <= D <= 1 << 20 and H <= 1 << 20, "a token has at most 2^20 heads, a head 1 .. 2^20 elements")
+    _need(1 <= D <= MAX_HEAD and H <= 1 << 20, "a token has at most 2^20 heads, a head 1 .. 2^20 elements")
     cs = None
     if table is not None:
         cs = _cs(table, interleaved, False, D, dev)
@@ -316,9 +317,10 @@ class _Linear(torch.autograd.Function):
         saved = kept.place(dev)[0] if kept.made else None
         with _on_device(dev):
             stream = _stream(None, dev)
-            if need_w:
+            if need_w or K > MAX_HEAD:   # (the same codes of longer rows than a head may have)
                 _check("gvr_fp8_quantize_matrix", L.gvr_fp8_quantize_matrix(
-                    x2.data_ptr(), x2.stride(0), DTYPES[x.dtype], M, K, ctypes.byref(xq), ctypes.byref(xt), 0, stream))
+                    x2.data_ptr(), x2.stride(0), DTYPES[x.dtype], M, K, ctypes.byref(xq),
+                    ctypes.byref(xt) if need_w else None, 0, stream))
             else:
                 _check("gvr_fp8_quantize", L.gvr_fp8_quantize(
                     ctypes.byref(_Heads(x2.data_ptr(), x2.stride(0), 0)), DTYPES[x.dtype], M, 1, K, None, None,
