@@ -111,7 +111,8 @@ gvr_status gvr_fp8_quantize_matrix(const void* x, int64_t x_stride, int32_t dtyp
  * result's own rounding unless terms cancel. Into float32 they are summed on the float16 matrix cores, where the
  * codes are exact, in float32 and at half the rate. Scales, blocks and splits are
  * float32 in both: off by about (K + 2 K / 128) 2^-24 of the magnitudes at most. The
- * result is rounded once.
+ * result is rounded once. Where terms cancel and the difference matters, ask for float32
+ * and round that to 16 bits.
  *
  * workspace: 16-byte aligned device memory of ws_bytes, used by this call only
  * while it runs (no clearing needed), for products whose sum is split over several

@@ -231,7 +231,9 @@ def gvr_fp8_matmul(a, a_scale, b, b_scale, out=None, dtype=torch.bfloat16, works
     """out [M][N] = A B^T of codes a uint8 [M][K] with a_scale float32 [M][K / 128]
     and codes b [N][K] with b_scale [N / 128][K / 128] (a weight in blocks of
     128 x 128) or [N][K / 128]; any row strides, any strides of the scales.
-    ``dtype``: bfloat16, float16 or float32, if ``out`` is not given.
+    ``dtype``: bfloat16, float16 or float32, if ``out`` is not given. Into 16 bits the
+    matrix cores cut products off at 2^-13 of the largest of eight neighbours
+    (``include/gvr_fp8.h``, Numerics); into float32 every sum is float32, at half the rate.
     ``workspace``: device memory for split sums (``gvr_fp8_matmul_workspace``
     bytes; allocated for the call if None). No gradient is recorded
     (``gvr_fp8_linear`` has one)."""
@@ -387,7 +389,8 @@ def gvr_fp8_linear(x, weight, weight_t=None):
     transposed=True)`` made, with that of W^T as ``weight_t``, which the gradient of
     x needs. x and the gradient of y are quantised by 128 elements along the axis
     that each product sums over; the rounding counts as the identity, and there is no
-    second derivative. y and the gradients have the types of x and of the weight.
+    second derivative. y and the gradients have the types of x and of the weight, and
+    their sums are those of ``gvr_fp8_matmul`` into that type.
     A training step may be captured into a graph, on one condition that all autograd
     nodes share: no graph that was recorded eagerly from the same leaves is alive
     (their accumulation belongs to the stream that it was recorded on)."""
