@@ -112,7 +112,10 @@ gvr_status gvr_fp8_quantize_matrix(const void* x, int64_t x_stride, int32_t dtyp
  * codes are exact, in float32 and at half the rate. Scales, blocks and splits are
  * float32 in both: off by about (K + 2 K / 128) 2^-24 of the magnitudes at most. The
  * result is rounded once. Where terms cancel and the difference matters, ask for float32
- * and round that to 16 bits.
+ * and round that to 16 bits. A block's sum is multiplied with the product of its two
+ * scales, which is a float32 number: below 2^-126 (the blocks' largest magnitudes
+ * multiply to less than 2^-108) it is rounded to a multiple of 2^-149, past 2^128 (more than
+ * 2^145) it is infinite, and the result then NaN where the sum of the codes' products is 0.
  *
  * workspace: 16-byte aligned device memory of ws_bytes, used by this call only
  * while it runs (no clearing needed), for products whose sum is split over several
